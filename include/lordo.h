@@ -299,6 +299,134 @@ LORDO_API int lordo_clip_coefficient_static(const void* G_dev, int g_dtype, int6
                                             void* stream);
 LORDO_API int64_t lordo_clip_coefficient_static_max_count(void);
 
+/* =============================================================================================
+ * Parameters outside the low-rank path: embedding tables, norm gains, biases.
+ *
+ * A model trained with the calls above has parameters that are no matrices of a context. They are updated by AdamW in a group of
+ * their own, for the same K workers held as replicas, and synchronised by the same outer step (the paper's comparison systems run
+ * Adam on every parameter; the low-rank path is defined for matrices only). Conventions are those at the top of this file: arrays
+ * are row-major, the replica axis is outermost, device memory belongs to the caller, calls enqueue on `stream` and return.
+ * Sizes need not be multiples of anything here.
+ * ============================================================================================= */
+
+typedef enum { LORDO_I32 = 0, LORDO_I64 = 1 } lordo_index;                     /* type of token arrays */
+typedef enum { LORDO_STATES_F32 = 0, LORDO_STATES_8BIT = 1 } lordo_states;
+
+/*
+ * Embedding lookup: out[k][t][:] = scale * W[k][tokens[k][t]][:], rounded once to out_dtype.
+ *   W       [K][V][d] in w_dtype (lordo_dtype)     tokens  [K][T] in `index` (lordo_index)     out  [K][T][d] in out_dtype
+ * A token outside [0, V) -- padding -- gives a row of zeros. T may be 0. K <= 64, V and T <= 2^30, d <= 2^24. Any element-aligned
+ * pointers; rows whose bytes are a multiple of 16, at 16-byte aligned addresses, are moved 16 bytes at a time. May be captured in a
+ * graph.
+ */
+LORDO_API int lordo_embedding(const void* W, int w_dtype, int K, int64_t V, int64_t d, const void* tokens, int index, int64_t T,
+                              float scale, void* out, int out_dtype, void* stream);
+
+/*
+ * Its gradient: dW[k][v][:] = scale * sum of dY[k][t][:] over the t with tokens[k][t] = v; accumulate = 1 adds that to dW, and rows
+ * whose token does not occur are left as they are (accumulate = 0: they become zero). dY is [K][T][d] in y_dtype, dW [K][V][d] in
+ * w_dtype. Tokens outside [0, V) take no part, whatever their rows of dY hold. Every sum is formed in fp32, in an order that depends
+ * on the tokens alone, and rounded once: the same bits on every run. `workspace` (256-byte aligned, size from the query, which makes
+ * no CUDA call) may be used by one call at a time. Limits as for lordo_embedding. May be captured in a graph.
+ */
+LORDO_API int lordo_embedding_grad_query_workspace(int K, int64_t V, int64_t d, int64_t T, size_t* bytes);
+LORDO_API int lordo_embedding_grad(const void* dY, int y_dtype, const void* tokens, int index, int K, int64_t V, int64_t d, int64_t T,
+                                   float scale, void* dW, int w_dtype, int accumulate, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+
+/* One tensor of an AdamW group. */
+typedef struct {
+  int64_t n;           /* elements (of one worker) */
+  int64_t row;         /* of a table whose gradient may be given by tokens: elements of a row, n a multiple; else 0 */
+  int64_t max_tokens;  /* with row > 0: most tokens of a worker in one step */
+  float weight_decay;
+  int32_t pad;         /* 0 */
+} lordo_tensor;
+
+typedef struct {
+  int32_t n_tensors;
+  const lordo_tensor* tensors; /* host array [n_tensors] */
+  int32_t K;                   /* workers held as replicas, 1 .. 64 */
+  int32_t w_dtype, g_dtype;    /* lordo_dtype */
+  int32_t states;              /* lordo_states: the moments in fp32, or in 8 bits (below) */
+  float beta2, eps;            /* eps > 0 */
+  float clip_rho;              /* clipping radius; <= 0 disables clipping */
+  int32_t clip_scope;          /* 0: one norm per worker over all tensors; 1: one per tensor */
+  int32_t sync;                /* 1: the group takes part in synchronisations (X0, B); 0: lordo_adamw_outer_step is refused */
+  int32_t sync_m, sync_v;      /* average the moments over workers in lordo_adamw_outer_step */
+  int32_t outer;               /* lordo_outer */
+  float outer_lr, outer_momentum;
+  uint64_t seed;               /* of the rounding of 8-bit moments */
+} lordo_adamw_config;
+
+/*
+ * Host tables of device pointers, one entry per tensor, 16-byte aligned.
+ *
+ * 8-bit moments: m and s = sqrt(v) are kept as OCP E4M3 codes, one scale per 256 consecutive elements of one worker's tensor (the last
+ * block of a worker may be shorter): value = code * 2^(scale byte - 127) (OCP E8M0). A scale puts the largest magnitude of its block
+ * into [128, 256), or is 2^-126 where that is smaller. A magnitude of t units of the scale's grid is rounded down after (u + 1/2) / 65536
+ * was added, u being 16 bits of the generator behind lordo_fill_random for (seed, step, tensor, worker, element): the expected value
+ * is the exact one, so averages with beta near 1, whose change in a step is a fraction of the distance between codes, keep moving.
+ * sqrt(v) > 0 never becomes 0 (the smallest code instead). The step itself uses the moments before they are rounded.
+ */
+typedef struct {
+  void* const* W;   /* [K][n] in w_dtype; on entry to lordo_adamw_init replica 0 holds the initial weights */
+  void* const* m;   /* [K][n] fp32, or E4M3 */
+  void* const* v;   /* [K][n] fp32, or E4M3 of sqrt(v) */
+  void* const* ms;  /* [K][ceil(n / 256)] E8M0, 8-bit moments only, else NULL */
+  void* const* vs;
+  float* const* X0; /* [n] model copy of the last synchronisation; NULL when sync == 0 */
+  float* const* B;  /* [n] outer momentum; NULL when sync == 0 or outer == LORDO_OUTER_AVG */
+} lordo_adamw_buffers;
+
+/* The gradient of one tensor in one step. */
+typedef struct {
+  const void* G;       /* [K][n] in g_dtype, 16-byte aligned; with tokens: [K][T][row], the gradient of the lookup's output */
+  const void* tokens;  /* NULL, or [K][T]: the gradient is scale * (sum of the rows of G that belong to each token), kept in fp32 */
+  int64_t T;           /* 0 <= T <= max_tokens */
+  int32_t index;       /* lordo_index */
+  float scale;
+} lordo_grad;
+
+typedef struct lordo_adamw_ctx lordo_adamw_ctx; /* opaque, host memory, library-owned */
+
+LORDO_API int lordo_adamw_query_workspace(const lordo_adamw_config* cfg, size_t* bytes); /* no CUDA call */
+
+/* Copies W[0] to every replica and to X0, zeroes the moments and B, synchronises `stream`. `workspace` is 256-byte aligned. */
+LORDO_API int lordo_adamw_init(const lordo_adamw_config* cfg, const lordo_adamw_buffers* buf, void* workspace, size_t workspace_bytes,
+                               void* stream, lordo_adamw_ctx** out);
+
+/*
+ * One step on every tensor and worker, G: host array [n_tensors]:
+ *   g = c_k G;  m <- beta1 m + (1-beta1) g;  v <- beta2 v + (1-beta2) g^2;  m^ = m / (1-beta1^s);  v^ = v / (1-beta2^s)
+ *   W <- W - lr ((omega m^ + (1-omega) g) / (sqrt(v^) + eps) + weight_decay W)
+ * omega = 1 is AdamW, omega < 1 the quasi-hyperbolic form of the low-rank path. c_k = min(1, rho / (norm + 1e-6)), or, with coef_dev
+ * (K floats in device memory), coef_dev[k]: for instance the coefficients of a lordo_ctx. s counts the steps of this context. A gradient
+ * norm that is NaN or infinite sets LORDO_FLAG_NONFINITE_GRAD (only where the norm is formed). The step count and the rates are host
+ * values, so a stream that is being captured is refused (LORDO_ERR_UNSUPPORTED).
+ */
+LORDO_API int lordo_adamw_step(lordo_adamw_ctx* ctx, const lordo_grad* G, float lr, float beta1, float omega, const float* coef_dev,
+                               void* stream);
+
+/*
+ * The synchronisation lines of Algorithm 1 for the group: m, v <- mean over the workers (sync_m, sync_v; 8-bit moments: the mean of v,
+ * rounded once, the same codes for every worker); D = X0 - mean_k W_k; averaging: X0 <- X0 - D; Nesterov: B <- mu_s B + D,
+ * X0 <- X0 - eta_s (D + mu_s B); every W_k <- X0. To be called wherever lordo_outer_step is; it keeps no schedule of its own. A stream that
+ * is being captured is refused.
+ */
+LORDO_API int lordo_adamw_outer_step(lordo_adamw_ctx* ctx, void* stream);
+
+LORDO_API int lordo_adamw_poll_status(lordo_adamw_ctx* ctx, void* stream, uint32_t* flags); /* as lordo_poll_status */
+LORDO_API int lordo_adamw_clear_status(lordo_adamw_ctx* ctx, void* stream);
+/* {steps done, synchronisations done}: with the caller's tensors, all that a checkpoint needs. */
+LORDO_API int lordo_adamw_get_counters(const lordo_adamw_ctx* ctx, int64_t out[2]);
+LORDO_API int lordo_adamw_set_counters(lordo_adamw_ctx* ctx, const int64_t in[2]);
+/* Device address of the clip coefficients of the last step that formed them, [n_tensors][K] fp32 (1 before that). */
+LORDO_API int lordo_adamw_clip_coefficients(const lordo_adamw_ctx* ctx, const float** device_ptr);
+LORDO_API int64_t lordo_adamw_launch_count(const lordo_adamw_ctx* ctx);
+LORDO_API const char* lordo_adamw_last_error(const lordo_adamw_ctx* ctx);
+LORDO_API int lordo_adamw_destroy(lordo_adamw_ctx* ctx);
+
 #ifdef __cplusplus
 }
 #endif

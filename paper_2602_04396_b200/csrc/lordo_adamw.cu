@@ -1,0 +1,565 @@
+// AdamW over many tensors at once, K workers' replicas each, with moments in 32 or in 8 bits:
+//   g = c_k G; m <- b1 m + (1-b1) g; v <- b2 v + (1-b2) g^2; m^ = m/(1-b1^s), v^ = v/(1-b2^s)
+//   W <- W - lr ((w m^ + (1-w) g) / (sqrt(v^) + eps) + wd W)
+// and the outer synchronisation of such tensors.
+#include "lordo_adamw.h"
+#include "lordo_kernels.h"
+
+namespace lordo {
+namespace {
+
+__device__ __forceinline__ int find_tensor(const unsigned* start, int count, unsigned x) {
+  int lo = 0, hi = count - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (start[mid] <= x) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+template <int DT>
+__device__ __forceinline__ void load8(const void* base, long long at, float (&x)[8]) {
+  if constexpr (DT == LORDO_F32) {
+    const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(base) + at);
+    const float4 a = p[0], b = p[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  } else {
+    const uint4 a = *reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned short*>(base) + at);
+    const unsigned r[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[2 * j] = __uint_as_float(r[j] << 16);
+      x[2 * j + 1] = __uint_as_float(r[j] & 0xFFFF0000u);
+    }
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ void store8(void* base, long long at, const float (&x)[8]) {
+  if constexpr (DT == LORDO_F32) {
+    float4* p = reinterpret_cast<float4*>(reinterpret_cast<float*>(base) + at);
+    p[0] = make_float4(x[0], x[1], x[2], x[3]);
+    p[1] = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+    uint4 a;
+    a.x = pack_bf16x2(x[0], x[1]); a.y = pack_bf16x2(x[2], x[3]); a.z = pack_bf16x2(x[4], x[5]); a.w = pack_bf16x2(x[6], x[7]);
+    *reinterpret_cast<uint4*>(reinterpret_cast<unsigned short*>(base) + at) = a;
+  }
+}
+
+// Gradient of element e of worker k of a table whose rows were summed by token.
+__device__ __forceinline__ float row_grad(const AwTensor& T, int k, long long e) {
+  const long long v = e / T.d;
+  const int2 seg = __ldg(T.segs + (long long)k * (T.n / T.d) + v);
+  return seg.x < seg.y ? T.rows[((long long)k * T.cap + seg.x) * T.d + (e - v * T.d)] : 0.f;
+}
+__device__ __forceinline__ void row_grad8(const AwTensor& T, int k, long long e, float (&g)[8]) {
+  if ((T.d & 7) == 0) {
+    const long long v = e / T.d;
+    const int2 seg = __ldg(T.segs + (long long)k * (T.n / T.d) + v);
+    if (seg.x < seg.y) {
+      load8<LORDO_F32>(T.rows, ((long long)k * T.cap + seg.x) * T.d + (e - v * T.d), g);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) g[j] = 0.f;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g[j] = row_grad(T, k, e + j);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Clip coefficients: partial sums of squares of chunks, one per block; the last block of a worker (scope 0) or of a tensor of a worker
+// (scope 1) adds its partial sums, in a fixed order whichever block it is.
+// ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ double block_sum(double x, double* red) {
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = x;
+  __syncthreads();
+  double s = 0.0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) s += red[w];
+  return s;
+}
+
+template <int GDT>
+__global__ void __launch_bounds__(256) adamw_norm_kernel(const __grid_constant__ AwTable tab, AwLaunch l, AwClip c) {
+  __shared__ double red[2][8];
+  __shared__ bool last_s;
+  const int t = threadIdx.x;
+  const int k = (int)(blockIdx.x / l.units);
+  const unsigned q = blockIdx.x - (unsigned)k * l.units;
+  const int i = find_tensor(tab.start, l.count, q);
+  const AwTensor& T = l.tensors[i];
+  const long long n = T.n;
+  const int index = T.index;
+  const void* G = tab.G[i];
+  dep_begin();
+  double s = 0.0;
+  if (G) {
+    const long long e0 = (long long)(q - tab.start[i]) * kAwChunk;
+    const long long e1 = e0 + kAwChunk < n ? e0 + kAwChunk : n;
+    const long long f0 = (long long)k * n + e0, f1 = (long long)k * n + e1;
+    const long long a0 = (f0 + 7) & ~7ll, a1 = f1 & ~7ll;
+    float sum[2] = {0.f, 0.f};
+    for (long long f = a0 + 8 * t; f < a1; f += 2 * 2048) {
+      float x[2][8];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (f + u * 2048 < a1) {
+          load8<GDT>(G, f + u * 2048, x[u]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[u][j] = 0.f;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[u] += x[u][j] * x[u][j];
+    }
+    s = (double)sum[0] + (double)sum[1];
+    const long long edge = t < 8 ? f0 + t : (a1 > a0 ? a1 : a0) + t - 8;  // elements before the first and behind the last vector
+    if (t < 16 && edge < f1 && (t >= 8 || edge < a0)) {
+      const float x = load1(G, GDT, edge);
+      s += (double)(x * x);
+    }
+  } else if (q == tab.start[i]) {  // its first chunk stands for the whole tensor
+    const int count = *T.rowsq_count;
+    const double* p = T.rowsq + (long long)k * count;
+    for (int x = t; x < count; x += 256) s += __ldcg(p + x);
+  }
+  s = block_sum(s, red[0]);
+  const unsigned first = c.scope ? c.at + tab.start[i] : 0u;
+  const unsigned many = c.scope ? tab.start[i + 1] - tab.start[i] : c.total;
+  if (t == 0) {
+    c.partial[(size_t)k * c.total + c.at + q] = s;
+    __threadfence();
+    unsigned* ticket = c.tickets + (c.scope ? (long long)index * l.K + k : k);
+    last_s = atomicInc(ticket, many - 1) == many - 1;  // back to zero with the last block
+  }
+  __syncthreads();
+  if (!last_s) return;
+  __threadfence();
+  const double* p = c.partial + (size_t)k * c.total + first;
+  double a = 0.0;
+  for (unsigned x = t; x < many; x += 256) a += __ldcg(p + x);
+  const double total = block_sum(a, red[1]);
+  if (t == 0 && !isfinite(total)) atomicOr(c.status, LORDO_FLAG_NONFINITE_GRAD);
+  const float coef = fminf(1.f, c.rho / ((float)sqrt(total) + 1e-6f));
+  if (c.scope) {
+    if (t == 0) c.coef[(long long)index * l.K + k] = coef;
+  } else {
+    for (int x = t; x < c.n_tensors; x += 256) c.coef[(long long)x * l.K + k] = coef;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Step, 32-bit moments
+// ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ void update(const AwStep& s, float wd, float c, float g, float& m, float& v, float& w) {
+  g *= c;
+  m = s.b1 * m + s.a1 * g;
+  v = s.b2 * v + s.a2 * g * g;
+  const float up = (s.omega * (m * s.inv_bc1) + s.a_omega * g) / (sqrtf(v * s.inv_bc2) + s.eps);
+  w -= s.lr * (up + wd * w);
+}
+
+template <int WDT, int GDT>
+__global__ void __launch_bounds__(256) adamw_step_kernel(const __grid_constant__ AwTable tab, AwLaunch l, const float* __restrict__ coef, int stride, AwStep s) {
+  const int t = threadIdx.x;
+  const int k = (int)(blockIdx.x / l.units);
+  const unsigned q = blockIdx.x - (unsigned)k * l.units;
+  const int i = find_tensor(tab.start, l.count, q);
+  const AwTensor T = l.tensors[i];
+  const void* G = tab.G[i];
+  dep_begin();
+  const float c = coef ? __ldcg(coef + (long long)T.index * stride + k) : 1.f;
+  const long long e0 = (long long)(q - tab.start[i]) * kAwPiece;
+  const long long e1 = e0 + kAwPiece < T.n ? e0 + kAwPiece : T.n;
+  const long long base = (long long)k * T.n, f0 = base + e0, f1 = base + e1;
+  const long long a0 = (f0 + 7) & ~7ll, a1 = f1 & ~7ll;
+  float* M = reinterpret_cast<float*>(T.m);
+  float* V = reinterpret_cast<float*>(T.v);
+  for (long long f = a0 + 8 * t; f < a1; f += 2048) {
+    float g[8], w[8], m[8], v[8];
+    if (G) load8<GDT>(G, f, g); else row_grad8(T, k, f - base, g);
+    load8<WDT>(T.W, f, w);
+    load8<LORDO_F32>(M, f, m);
+    load8<LORDO_F32>(V, f, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) update(s, T.wd, c, g[j], m[j], v[j], w[j]);
+    store8<LORDO_F32>(M, f, m);
+    store8<LORDO_F32>(V, f, v);
+    store8<WDT>(T.W, f, w);
+  }
+  const long long edge = t < 8 ? f0 + t : (a1 > a0 ? a1 : a0) + t - 8;
+  if (t < 16 && edge < f1 && (t >= 8 || edge < a0)) {
+    const float g = G ? load1(G, GDT, edge) : row_grad(T, k, edge - base);
+    float w = load1(T.W, WDT, edge), m = M[edge], v = V[edge];
+    update(s, T.wd, c, g, m, v, w);
+    M[edge] = m;
+    V[edge] = v;
+    store1(T.W, WDT, edge, w);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// 8-bit moments: E4M3 codes of m and of sqrt(v), a power of two per block of 256 as their scale, rounded up or down at random.
+// Rounded to the nearest the averages would stand still: b2 = 0.999 moves v by 0.1 % a step, and codes are 6 to 12 % apart. With powers
+// of two for scales a value stays where it is on the grid when the largest of its block changes; an fp32 scale (the largest itself) would
+// move all 256 off the grid in every step, and the noise of rounding them again would add up. sqrt(v) has half the range of v.
+// ---------------------------------------------------------------------------------------------
+// 16 random bits for each of four consecutive elements
+__device__ __forceinline__ unsigned long long bits4(unsigned long long key, long long e) { return mix64(key + kGolden * (unsigned long long)((e >> 2) + 1)); }
+
+// Exponent byte of the scale that puts `top` (the bits of a magnitude) into [128, 256) times itself.
+__device__ __forceinline__ int scale_code(unsigned top) {
+  const int e = (int)(top >> 23) - 7;
+  return e < 1 ? 1 : e;
+}
+__device__ __forceinline__ float pow2(int code) { return __int_as_float(code << 23); }  // 2^(code - 127), code in [1, 254]
+
+// E4M3 code of a magnitude t < 256, rounded down after (u + 1/2) / 65536 of a step was added. Below 2^-6 the steps are 2^-9 wide, as they
+// are for t + 2^-6. Infinities and NaN become NaN.
+__device__ __forceinline__ int code8(float t, unsigned u) {
+  const bool sub = t < 0.015625f;
+  const unsigned b = __float_as_uint(fabsf(sub ? t + 0.015625f : t));
+  const int code = (int)((b + (u << 4) + 8u) >> 20) - (sub ? 968 : 960);
+  return code > 127 ? 127 : code;
+}
+__device__ __forceinline__ float value8(unsigned byte) {  // of an E4M3 code
+  const unsigned e = byte & 0x7Fu;
+  float x = __uint_as_float((e << 20)) * __uint_as_float(0x7B800000u);  // 2^120: moves the exponent's bias, subnormals too
+  if (e == 127u) x = __uint_as_float(0x7FC00000u);
+  return byte & 0x80u ? -x : x;
+}
+
+template <int WDT, int GDT>
+__global__ void __launch_bounds__(256) adamw_step8_kernel(const __grid_constant__ AwTable tab, AwLaunch l, const float* __restrict__ coef, int stride, AwStep s) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int k = (int)(blockIdx.x / l.units);
+  const unsigned q = blockIdx.x - (unsigned)k * l.units;
+  const int i = find_tensor(tab.start, l.count, q);
+  const AwTensor T = l.tensors[i];
+  const void* G = tab.G[i];
+  const unsigned long long key = mix64(s.key + kGolden * ((unsigned long long)T.index * l.K + k + 1));
+  dep_begin();
+  const float c = coef ? __ldcg(coef + (long long)T.index * stride + k) : 1.f;
+  const long long base = (long long)k * T.n;
+  unsigned char* M = reinterpret_cast<unsigned char*>(T.m);
+  unsigned char* V = reinterpret_cast<unsigned char*>(T.v);
+  const long long b0 = (long long)(q - tab.start[i]) * (kAwPiece / kAwBlock);
+  for (int x = warp; x < kAwPiece / kAwBlock; x += 8) {
+    const long long b = b0 + x;
+    if (b >= T.nb) break;
+    const long long e = b * kAwBlock + 8 * lane, f = base + e;
+    const bool vec = ((base & 7) == 0) && e + 8 <= T.n;
+    const int left = e >= T.n ? 0 : T.n - e < 8 ? (int)(T.n - e) : 8;
+    float g[8], w[8], m[8], v[8];
+    unsigned mc[2] = {0u, 0u}, vc[2] = {0u, 0u};
+    if (vec) {
+      if (G) load8<GDT>(G, f, g); else row_grad8(T, k, e, g);
+      load8<WDT>(T.W, f, w);
+      const uint2 a = *reinterpret_cast<const uint2*>(M + f), d = *reinterpret_cast<const uint2*>(V + f);
+      mc[0] = a.x; mc[1] = a.y; vc[0] = d.x; vc[1] = d.y;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        g[j] = w[j] = 0.f;
+        if (j < left) {
+          g[j] = G ? load1(G, GDT, f + j) : row_grad(T, k, e + j);
+          w[j] = load1(T.W, WDT, f + j);
+          mc[j >> 2] |= (unsigned)M[f + j] << (8 * (j & 3));
+          vc[j >> 2] |= (unsigned)V[f + j] << (8 * (j & 3));
+        }
+      }
+    }
+    const long long sb = (long long)k * T.nb + b;
+    const float ms = pow2(T.ms[sb]), vs = pow2(T.vs[sb]);
+    unsigned mtop = 0u, vtop = 0u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      m[j] = value8((mc[j >> 2] >> (8 * (j & 3))) & 0xFFu) * ms;
+      const float r = value8((vc[j >> 2] >> (8 * (j & 3))) & 0xFFu) * vs;
+      v[j] = r * r;
+      update(s, T.wd, c, g[j], m[j], v[j], w[j]);
+      v[j] = sqrtf(v[j]);
+      const unsigned ma = __float_as_uint(m[j]) & 0x7FFFFFFFu, va = __float_as_uint(v[j]);
+      mtop = ma > mtop ? ma : mtop;
+      vtop = va > vtop ? va : vtop;
+    }
+    const int mcode = scale_code(__reduce_max_sync(0xffffffffu, mtop)), vcode = scale_code(__reduce_max_sync(0xffffffffu, vtop));
+    const float mi = pow2(254 - mcode), vi = pow2(254 - vcode);
+    mc[0] = mc[1] = vc[0] = vc[1] = 0u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const unsigned long long r = bits4(key, e + 4 * h);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const unsigned u = (unsigned)(r >> (16 * j)) & 0xFFFFu;
+        const float x = m[4 * h + j], y = v[4 * h + j];
+        const unsigned a = (unsigned)code8(fabsf(x) * mi, u) | ((__float_as_uint(x) >> 24) & 0x80u);
+        unsigned d = (unsigned)code8(y * vi, (u * 40503u) & 0xFFFFu);
+        if (d == 0u && y > 0.f) d = 1u;
+        mc[h] |= a << (8 * j);
+        vc[h] |= d << (8 * j);
+      }
+    }
+    if (vec) {
+      store8<WDT>(T.W, f, w);
+      *reinterpret_cast<uint2*>(M + f) = make_uint2(mc[0], mc[1]);
+      *reinterpret_cast<uint2*>(V + f) = make_uint2(vc[0], vc[1]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (j < left) {
+          store1(T.W, WDT, f + j, w[j]);
+          M[f + j] = (unsigned char)(mc[j >> 2] >> (8 * (j & 3)));
+          V[f + j] = (unsigned char)(vc[j >> 2] >> (8 * (j & 3)));
+        }
+      }
+    }
+    __syncwarp();  // every lane has read the scales
+    if (lane == 0) {
+      T.ms[sb] = (unsigned char)mcode;
+      T.vs[sb] = (unsigned char)vcode;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Outer synchronisation: moments <- mean over the workers; D = X0 - mean W; average: X0 <- X0 - D; Nesterov: B <- mu B + D,
+// X0 <- X0 - eta (D + mu B); every W_k <- X0.
+// ---------------------------------------------------------------------------------------------
+template <int WDT, int N>  // N consecutive elements of every worker: 4 (a float4's alignment everywhere) or 1
+__device__ __forceinline__ void outer_weights(const AwTensor& T, int K, const AwOuter& o, float inv_k, long long e) {
+  float s[N] = {}, x0[N], b[N];
+#pragma unroll 4
+  for (int k = 0; k < K; ++k) {
+    if constexpr (N == 4) {
+      const float4 w = load4(T.W, WDT, (long long)k * T.n + e);
+      s[0] += w.x; s[1] += w.y; s[2] += w.z; s[3] += w.w;
+    } else {
+      s[0] += load1(T.W, WDT, (long long)k * T.n + e);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    x0[j] = T.X0[e + j];
+    const float d = x0[j] - s[j] * inv_k;
+    if (o.nesterov) {
+      b[j] = o.mu * T.B[e + j] + d;
+      x0[j] -= o.eta * (d + o.mu * b[j]);
+    } else {
+      x0[j] -= d;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    T.X0[e + j] = x0[j];
+    if (o.nesterov) T.B[e + j] = b[j];
+  }
+#pragma unroll 4
+  for (int k = 0; k < K; ++k) {
+    if constexpr (N == 4) store4(T.W, WDT, (long long)k * T.n + e, make_float4(x0[0], x0[1], x0[2], x0[3]));
+    else store1(T.W, WDT, (long long)k * T.n + e, x0[0]);
+  }
+}
+
+template <int N>
+__device__ __forceinline__ void outer_mean(float* p, long long n, int K, float inv_k, long long e) {
+  float s[N] = {};
+#pragma unroll 4
+  for (int k = 0; k < K; ++k) {
+    if constexpr (N == 4) {
+      const float4 x = *reinterpret_cast<const float4*>(p + (long long)k * n + e);
+      s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
+    } else {
+      s[0] += p[(long long)k * n + e];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) s[j] *= inv_k;
+#pragma unroll 4
+  for (int k = 0; k < K; ++k) {
+    if constexpr (N == 4) *reinterpret_cast<float4*>(p + (long long)k * n + e) = make_float4(s[0], s[1], s[2], s[3]);
+    else p[(long long)k * n + e] = s[0];
+  }
+}
+
+template <int WDT>
+__global__ void __launch_bounds__(256) adamw_outer_kernel(AwLaunch l, const unsigned* __restrict__ start, AwOuter o) {
+  const int i = find_tensor(start, l.count, blockIdx.x);
+  const AwTensor T = l.tensors[i];
+  dep_begin();
+  const float inv_k = 1.f / (float)l.K;
+  const long long e0 = (long long)(blockIdx.x - start[i]) * kAwOuter;
+  const long long e1 = e0 + kAwOuter < T.n ? e0 + kAwOuter : T.n;
+  if (T.n % 4 == 0) {
+    for (long long e = e0 + 4 * threadIdx.x; e < e1; e += 1024) {
+      outer_weights<WDT, 4>(T, l.K, o, inv_k, e);
+      if (o.sync_m) outer_mean<4>(reinterpret_cast<float*>(T.m), T.n, l.K, inv_k, e);
+      if (o.sync_v) outer_mean<4>(reinterpret_cast<float*>(T.v), T.n, l.K, inv_k, e);
+    }
+  } else {
+    for (long long e = e0 + threadIdx.x; e < e1; e += 256) {
+      outer_weights<WDT, 1>(T, l.K, o, inv_k, e);
+      if (o.sync_m) outer_mean<1>(reinterpret_cast<float*>(T.m), T.n, l.K, inv_k, e);
+      if (o.sync_v) outer_mean<1>(reinterpret_cast<float*>(T.v), T.n, l.K, inv_k, e);
+    }
+  }
+}
+
+// Mean over the workers of one array of 8-bit moments, one block of 256 of every worker: a lane has eight elements.
+template <bool SECOND>
+__device__ __forceinline__ void outer_mean8(const AwTensor& T, int K, float inv_k, unsigned long long key, long long b, long long e, int left, int lane) {
+  unsigned char* C = reinterpret_cast<unsigned char*>(SECOND ? T.v : T.m);
+  unsigned char* S = SECOND ? T.vs : T.ms;
+  const bool vec = left == 8 && (T.n & 7) == 0;
+  float a[8] = {};
+  for (int k = 0; k < K; ++k) {
+    const float scale = pow2(S[(long long)k * T.nb + b]);
+    const unsigned char* p = C + (long long)k * T.n + e;
+    unsigned c[2] = {0u, 0u};
+    if (vec) {
+      const uint2 x = *reinterpret_cast<const uint2*>(p);
+      c[0] = x.x; c[1] = x.y;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < left) c[j >> 2] |= (unsigned)p[j] << (8 * (j & 3));
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float x = value8((c[j >> 2] >> (8 * (j & 3))) & 0xFFu) * scale;
+      a[j] += SECOND ? x * x : x;
+    }
+  }
+  unsigned top = 0u;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    a[j] *= inv_k;
+    if (SECOND) a[j] = sqrtf(a[j]);
+    const unsigned x = __float_as_uint(a[j]) & 0x7FFFFFFFu;
+    top = x > top ? x : top;
+  }
+  const int code = scale_code(__reduce_max_sync(0xffffffffu, top));
+  const float inv = pow2(254 - code);
+  unsigned c[2] = {0u, 0u};
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const unsigned long long r = bits4(key, e + 4 * h);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      unsigned u = (unsigned)(r >> (16 * j)) & 0xFFFFu;
+      if (SECOND) u = (u * 40503u) & 0xFFFFu;
+      const float x = a[4 * h + j];
+      unsigned y = (unsigned)code8(fabsf(x) * inv, u);
+      if (SECOND) { if (y == 0u && x > 0.f) y = 1u; }
+      else y |= (__float_as_uint(x) >> 24) & 0x80u;
+      c[h] |= y << (8 * j);
+    }
+  }
+  for (int k = 0; k < K; ++k) {
+    unsigned char* p = C + (long long)k * T.n + e;
+    if (vec) {
+      *reinterpret_cast<uint2*>(p) = make_uint2(c[0], c[1]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < left) p[j] = (unsigned char)(c[j >> 2] >> (8 * (j & 3)));
+    }
+  }
+  __syncwarp();  // every lane has read the scales
+  for (int k = lane; k < K; k += 32) S[(long long)k * T.nb + b] = (unsigned char)code;
+}
+
+template <int WDT>
+__global__ void __launch_bounds__(256) adamw_outer8_kernel(AwLaunch l, const unsigned* __restrict__ start, AwOuter o) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int i = find_tensor(start, l.count, blockIdx.x);
+  const AwTensor T = l.tensors[i];
+  const unsigned long long key = mix64(o.key + kGolden * ((unsigned long long)T.index + 1));
+  dep_begin();
+  const float inv_k = 1.f / (float)l.K;
+  const long long b0 = (long long)(blockIdx.x - start[i]) * (kAwOuter / kAwBlock);
+  for (int x = warp; x < kAwOuter / kAwBlock; x += 8) {
+    const long long b = b0 + x;
+    if (b >= T.nb) break;
+    const long long at = b * kAwBlock, e = at + 8 * lane;
+    const int left = e >= T.n ? 0 : T.n - e < 8 ? (int)(T.n - e) : 8;
+    if (T.n % 4 == 0) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (at + 128 * h + 4 * lane < T.n) outer_weights<WDT, 4>(T, l.K, o, inv_k, at + 128 * h + 4 * lane);
+    } else {
+      for (int j = lane; j < kAwBlock && at + j < T.n; j += 32) outer_weights<WDT, 1>(T, l.K, o, inv_k, at + j);
+    }
+    if (o.sync_m) outer_mean8<false>(T, l.K, inv_k, key, b, e, left, lane);
+    if (o.sync_v) outer_mean8<true>(T, l.K, inv_k, key, b, e, left, lane);
+  }
+}
+
+__global__ void __launch_bounds__(256) adamw_init_kernel(AwLaunch l, const unsigned* __restrict__ start) {
+  const int i = find_tensor(start, l.count, blockIdx.x);
+  const AwTensor T = l.tensors[i];
+  const long long e0 = (long long)(blockIdx.x - start[i]) * kAwOuter;
+  const long long e1 = e0 + kAwOuter < T.n ? e0 + kAwOuter : T.n;
+  for (long long e = e0 + threadIdx.x; e < e1; e += 256) {
+    const float w = load1(T.W, l.w_dt, e);
+    if (T.X0) T.X0[e] = w;
+    if (T.B) T.B[e] = 0.f;
+    for (int k = 0; k < l.K; ++k) {
+      const long long f = (long long)k * T.n + e;
+      if (k) store1(T.W, l.w_dt, f, w);
+      if (l.small) {
+        reinterpret_cast<unsigned char*>(T.m)[f] = 0;
+        reinterpret_cast<unsigned char*>(T.v)[f] = 0;
+        if (e % kAwBlock == 0) T.ms[(long long)k * T.nb + e / kAwBlock] = T.vs[(long long)k * T.nb + e / kAwBlock] = 1;
+      } else {
+        reinterpret_cast<float*>(T.m)[f] = 0.f;
+        reinterpret_cast<float*>(T.v)[f] = 0.f;
+      }
+    }
+  }
+}
+
+}  // namespace
+
+void launch_aw_norm(const AwLaunch& l, const AwTable& t, const AwClip& c, cudaStream_t st) {
+  const dim3 grid(l.units * (unsigned)l.K);
+  if (l.g_dt == LORDO_F32) launch_dep(adamw_norm_kernel<LORDO_F32>, grid, 256, 0, st, t, l, c);
+  else launch_dep(adamw_norm_kernel<LORDO_BF16>, grid, 256, 0, st, t, l, c);
+}
+
+void launch_aw_step(const AwLaunch& l, const AwTable& t, const float* coef, int stride, const AwStep& s, cudaStream_t st) {
+  const dim3 grid(l.units * (unsigned)l.K);
+#define LORDO_AW(W, G)                                                                              \
+  if (l.small) launch_dep(adamw_step8_kernel<W, G>, grid, 256, 0, st, t, l, coef, stride, s);       \
+  else launch_dep(adamw_step_kernel<W, G>, grid, 256, 0, st, t, l, coef, stride, s)
+  if (l.w_dt == LORDO_F32) {
+    if (l.g_dt == LORDO_F32) { LORDO_AW(LORDO_F32, LORDO_F32); } else { LORDO_AW(LORDO_F32, LORDO_BF16); }
+  } else {
+    if (l.g_dt == LORDO_F32) { LORDO_AW(LORDO_BF16, LORDO_F32); } else { LORDO_AW(LORDO_BF16, LORDO_BF16); }
+  }
+#undef LORDO_AW
+}
+
+void launch_aw_outer(const AwLaunch& l, const unsigned* start, const AwOuter& o, cudaStream_t st) {
+  const dim3 grid(l.units);
+  if (l.small) {
+    if (l.w_dt == LORDO_F32) launch_dep(adamw_outer8_kernel<LORDO_F32>, grid, 256, 0, st, l, start, o);
+    else launch_dep(adamw_outer8_kernel<LORDO_BF16>, grid, 256, 0, st, l, start, o);
+  } else {
+    if (l.w_dt == LORDO_F32) launch_dep(adamw_outer_kernel<LORDO_F32>, grid, 256, 0, st, l, start, o);
+    else launch_dep(adamw_outer_kernel<LORDO_BF16>, grid, 256, 0, st, l, start, o);
+  }
+}
+
+void launch_aw_init(const AwLaunch& l, const unsigned* start, cudaStream_t st) {
+  adamw_init_kernel<<<l.units, 256, 0, st>>>(l, start);
+}
+
+}  // namespace lordo

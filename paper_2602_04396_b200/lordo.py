@@ -26,6 +26,9 @@ EXPORTS = [
     "lordo_clip_coefficients", "lordo_launch_count", "lordo_last_error", "lordo_status_string", "lordo_destroy",
     "lordo_fill_random", "lordo_profile_enable", "lordo_profile_read", "lordo_clip_coefficient_static",
     "lordo_clip_coefficient_static_max_count", "lordo_clear_status", "lordo_selftest_wait_timeout", "lordo_diagnostics", "lordo_sync_states",
+    "lordo_embedding", "lordo_embedding_grad", "lordo_embedding_grad_query_workspace", "lordo_adamw_query_workspace", "lordo_adamw_init",
+    "lordo_adamw_step", "lordo_adamw_outer_step", "lordo_adamw_poll_status", "lordo_adamw_clear_status", "lordo_adamw_get_counters",
+    "lordo_adamw_set_counters", "lordo_adamw_clip_coefficients", "lordo_adamw_launch_count", "lordo_adamw_last_error", "lordo_adamw_destroy",
 ]
 
 
@@ -52,6 +55,27 @@ class _Config(C.Structure):
 
 class _Buffers(C.Structure):
     _fields_ = [(name, C.POINTER(C.c_void_p)) for name in ("W", "E", "P", "u", "v", "X0", "B", "Delta")]
+
+
+class _Tensor(C.Structure):
+    _fields_ = [("n", C.c_int64), ("row", C.c_int64), ("max_tokens", C.c_int64), ("weight_decay", C.c_float), ("pad", C.c_int32)]
+
+
+class _AdamWConfig(C.Structure):
+    _fields_ = [
+        ("n_tensors", C.c_int32), ("tensors", C.POINTER(_Tensor)), ("K", C.c_int32), ("w_dtype", C.c_int32), ("g_dtype", C.c_int32),
+        ("states", C.c_int32), ("beta2", C.c_float), ("eps", C.c_float), ("clip_rho", C.c_float), ("clip_scope", C.c_int32),
+        ("sync", C.c_int32), ("sync_m", C.c_int32), ("sync_v", C.c_int32), ("outer", C.c_int32), ("outer_lr", C.c_float),
+        ("outer_momentum", C.c_float), ("seed", C.c_uint64),
+    ]
+
+
+class _AdamWBuffers(C.Structure):
+    _fields_ = [(name, C.POINTER(C.c_void_p)) for name in ("W", "m", "v", "ms", "vs", "X0", "B")]
+
+
+class _Grad(C.Structure):
+    _fields_ = [("G", C.c_void_p), ("tokens", C.c_void_p), ("T", C.c_int64), ("index", C.c_int32), ("scale", C.c_float)]
 
 
 _lib = None
@@ -93,6 +117,23 @@ def load_library() -> C.CDLL:
     lib.lordo_clip_coefficient_static.argtypes = [vp, i32, i64, f32, vp, vp]
     lib.lordo_clip_coefficient_static_max_count.argtypes = []
     lib.lordo_clip_coefficient_static_max_count.restype = i64
+    lib.lordo_embedding.argtypes = [vp, i32, i32, i64, i64, vp, i32, i64, f32, vp, i32, vp]
+    lib.lordo_embedding_grad_query_workspace.argtypes = [i32, i64, i64, i64, C.POINTER(C.c_size_t)]
+    lib.lordo_embedding_grad.argtypes = [vp, i32, vp, i32, i32, i64, i64, i64, f32, vp, i32, i32, vp, C.c_size_t, vp]
+    lib.lordo_adamw_query_workspace.argtypes = [C.POINTER(_AdamWConfig), C.POINTER(C.c_size_t)]
+    lib.lordo_adamw_init.argtypes = [C.POINTER(_AdamWConfig), C.POINTER(_AdamWBuffers), vp, C.c_size_t, vp, C.POINTER(vp)]
+    lib.lordo_adamw_step.argtypes = [vp, C.POINTER(_Grad), f32, f32, f32, vp, vp]
+    lib.lordo_adamw_outer_step.argtypes = [vp, vp]
+    lib.lordo_adamw_poll_status.argtypes = [vp, vp, C.POINTER(C.c_uint32)]
+    lib.lordo_adamw_clear_status.argtypes = [vp, vp]
+    lib.lordo_adamw_get_counters.argtypes = [vp, C.POINTER(i64)]
+    lib.lordo_adamw_set_counters.argtypes = [vp, C.POINTER(i64)]
+    lib.lordo_adamw_clip_coefficients.argtypes = [vp, C.POINTER(vp)]
+    lib.lordo_adamw_launch_count.argtypes = [vp]
+    lib.lordo_adamw_launch_count.restype = i64
+    lib.lordo_adamw_last_error.argtypes = [vp]
+    lib.lordo_adamw_last_error.restype = C.c_char_p
+    lib.lordo_adamw_destroy.argtypes = [vp]
     for name in EXPORTS:
         if getattr(lib, name).restype is C.c_int:
             getattr(lib, name).restype = C.c_int
