@@ -339,8 +339,7 @@ typedef struct {
   int64_t n;           /* elements (of one worker) */
   int64_t row;         /* of a table whose gradient may be given by tokens: elements of a row, n a multiple; else 0 */
   int64_t max_tokens;  /* with row > 0: most tokens of a worker in one step */
-  float weight_decay;
-  int32_t pad;         /* 0 */
+  double weight_decay;
 } lordo_tensor;
 
 typedef struct {
@@ -349,13 +348,13 @@ typedef struct {
   int32_t K;                   /* workers held as replicas, 1 .. 64 */
   int32_t w_dtype, g_dtype;    /* lordo_dtype */
   int32_t states;              /* lordo_states: the moments in fp32, or in 8 bits (below) */
-  float beta2, eps;            /* eps > 0 */
-  float clip_rho;              /* clipping radius; <= 0 disables clipping */
+  double beta2, eps;           /* eps > 0. Rates are doubles here: 1 - 0.999f is 1.3e-5 off 0.001 */
+  double clip_rho;             /* clipping radius; <= 0 disables clipping */
   int32_t clip_scope;          /* 0: one norm per worker over all tensors; 1: one per tensor */
   int32_t sync;                /* 1: the group takes part in synchronisations (X0, B); 0: lordo_adamw_outer_step is refused */
   int32_t sync_m, sync_v;      /* average the moments over workers in lordo_adamw_outer_step */
   int32_t outer;               /* lordo_outer */
-  float outer_lr, outer_momentum;
+  double outer_lr, outer_momentum;
   uint64_t seed;               /* of the rounding of 8-bit moments */
 } lordo_adamw_config;
 
@@ -405,7 +404,7 @@ LORDO_API int lordo_adamw_init(const lordo_adamw_config* cfg, const lordo_adamw_
  * norm that is NaN or infinite sets LORDO_FLAG_NONFINITE_GRAD (only where the norm is formed). The step count and the rates are host
  * values, so a stream that is being captured is refused (LORDO_ERR_UNSUPPORTED).
  */
-LORDO_API int lordo_adamw_step(lordo_adamw_ctx* ctx, const lordo_grad* G, float lr, float beta1, float omega, const float* coef_dev,
+LORDO_API int lordo_adamw_step(lordo_adamw_ctx* ctx, const lordo_grad* G, double lr, double beta1, double omega, const float* coef_dev,
                                void* stream);
 
 /*

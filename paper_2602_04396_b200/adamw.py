@@ -10,6 +10,7 @@
 from __future__ import annotations
 
 import ctypes as C
+from array import array
 from typing import Dict, List, NamedTuple, Optional, Sequence, Union
 
 import torch
@@ -70,7 +71,7 @@ class AdamW:
             if not 0 <= i < len(W0) or len(self.shapes[i]) != 2 or most < 0:
                 raise ValueError("tables: {number of a two-dimensional tensor: most tokens} is wanted")
         self._tensors = (_Tensor * len(n))(*[
-            _Tensor(c, self.shapes[i][1] if i in self.tables else 0, self.tables.get(i, 0), decay[i], 0) for i, c in enumerate(n)])
+            _Tensor(c, self.shapes[i][1] if i in self.tables else 0, self.tables.get(i, 0), decay[i]) for i, c in enumerate(n)])
         small = states == "8bit"
         self.cfg = _AdamWConfig(len(n), self._tensors, self.K, _dtype_code(w_dtype), _dtype_code(self.g_dtype), _STATES[states], beta2, eps, clip_rho,
                                 clip_scope, int(outer is not None), int(sync_m), int(sync_v), lordo.OUTER_AVG if outer is None else outer,
@@ -114,7 +115,10 @@ class AdamW:
         if rc != 0:
             raise LordoError(rc, "lordo_adamw_init", self.lib.lordo_status_string(rc).decode())
         self._grads = (_Grad * len(n))()
-        self._full = [(self.K,) + s for s in self.shapes]
+        words = memoryview(self._grads).cast("B").cast("Q")  # four to a gradient, the first two its addresses
+        self._grad_at, self._tokens_at = words[0::4], words[1::4]
+        self._no_tokens = memoryview(array("Q", bytes(8 * len(n))))
+        self._full = [torch.Size((self.K,) + s) for s in self.shapes]
         self._keep = None
 
     # -- helpers -----------------------------------------------------------------------------
@@ -125,7 +129,8 @@ class AdamW:
     def _stream(self, stream: Optional[torch.cuda.Stream]) -> int:
         return (stream if stream is not None else torch.cuda.current_stream(self.device)).cuda_stream
 
-    def _token_grad(self, i: int, g: TokenGrad) -> _Grad:
+    def _token_grad(self, i: int, g: TokenGrad) -> int:
+        """Fills the gradient's entry but for the address of dY, which is returned."""
         tokens, dY, scale = g
         if i not in self.tables:
             raise ValueError(f"gradient {i}: tensor {i} is not among the tables")
@@ -135,10 +140,11 @@ class AdamW:
             raise ValueError(f"gradient {i}: tokens [K, ...] and dY of their shape + (d,) are wanted")
         if tokens.device != self.device or dY.device != self.device or not tokens.is_contiguous() or not dY.is_contiguous():
             raise ValueError(f"gradient {i}: contiguous tensors on {self.device} are wanted")
-        T = tokens.numel() // self.K
-        if T == 0:  # an empty tensor has no address, and without tokens the gradient would be a dense one
-            return _Grad(self.workspace.data_ptr(), self.workspace.data_ptr(), 0, _INDEX[tokens.dtype], scale)
-        return _Grad(dY.data_ptr(), tokens.data_ptr(), T, _INDEX[tokens.dtype], scale)
+        e = self._grads[i]
+        e.T, e.index, e.scale = tokens.numel() // self.K, _INDEX[tokens.dtype], scale
+        # an empty tensor has no address, and without tokens the gradient would be a dense one
+        e.tokens = tokens.data_ptr() if e.T else self.workspace.data_ptr()
+        return dY.data_ptr() if e.T else self.workspace.data_ptr()
 
     # -- calls -------------------------------------------------------------------------------
     def step(self, G: Sequence[Union[torch.Tensor, TokenGrad]], lr: float, beta1: float = 0.9, omega: float = 1.0,
@@ -147,19 +153,20 @@ class AdamW:
         group's own (for instance those of a Lordo)."""
         if len(G) != len(self.shapes):
             raise ValueError(f"{len(self.shapes)} gradients are wanted, not {len(G)}")
-        table, dt, dev = self._grads, self.g_dtype, self.device
-        for i, g in enumerate(G):
-            if isinstance(g, TokenGrad):
-                table[i] = self._token_grad(i, g)
-                continue
-            if g.shape != self._full[i] or g.dtype != dt or g.device != dev or not g.is_contiguous():
-                raise ValueError(f"gradient {i}: a contiguous {self._full[i]} tensor in {dt} on {dev} is wanted")
-            e = table[i]
-            e.G, e.tokens = g.data_ptr(), None
-        if coef is not None and (coef.dtype != torch.float32 or coef.numel() != self.K or coef.device != dev or not coef.is_contiguous()):
-            raise ValueError(f"coef: {self.K} contiguous float32 values on {dev} are wanted")
+        dt, index, at = self.g_dtype, self.device.index, array("Q")
+        self._tokens_at[:] = self._no_tokens
+        for g, shape in zip(G, self._full):
+            if g.__class__ is TokenGrad:
+                at.append(self._token_grad(len(at), g))
+            elif g.shape != shape or g.dtype is not dt or g.get_device() != index or not g.is_contiguous():
+                raise ValueError(f"gradient {len(at)}: a contiguous {tuple(shape)} tensor in {dt} on {self.device} is wanted")
+            else:
+                at.append(g.data_ptr())
+        self._grad_at[:] = memoryview(at)
+        if coef is not None and (coef.dtype != torch.float32 or coef.numel() != self.K or coef.device != self.device or not coef.is_contiguous()):
+            raise ValueError(f"coef: {self.K} contiguous float32 values on {self.device} are wanted")
         self._keep = (list(G), coef)  # alive until the next step: `stream` need not be the one they were allocated on
-        self._check(self._run(self.lib.lordo_adamw_step, table, lr, beta1, omega, coef.data_ptr() if coef is not None else None, self._stream(stream)),
+        self._check(self._run(self.lib.lordo_adamw_step, self._grads, lr, beta1, omega, coef.data_ptr() if coef is not None else None, self._stream(stream)),
                     "lordo_adamw_step")
 
     def _run(self, call, *args) -> int:

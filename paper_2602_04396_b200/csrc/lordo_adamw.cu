@@ -2,6 +2,9 @@
 //   g = c_k G; m <- b1 m + (1-b1) g; v <- b2 v + (1-b2) g^2; m^ = m/(1-b1^s), v^ = v/(1-b2^s)
 //   W <- W - lr ((w m^ + (1-w) g) / (sqrt(v^) + eps) + wd W)
 // and the outer synchronisation of such tensors.
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
 #include "lordo_adamw.h"
 #include "lordo_kernels.h"
 
@@ -102,7 +105,6 @@ __global__ void __launch_bounds__(256) adamw_norm_kernel(const __grid_constant__
     const long long e1 = e0 + kAwChunk < n ? e0 + kAwChunk : n;
     const long long f0 = (long long)k * n + e0, f1 = (long long)k * n + e1;
     const long long a0 = (f0 + 7) & ~7ll, a1 = f1 & ~7ll;
-    float sum[2] = {0.f, 0.f};
     for (long long f = a0 + 8 * t; f < a1; f += 2 * 2048) {
       float x[2][8];
 #pragma unroll
@@ -115,15 +117,17 @@ __global__ void __launch_bounds__(256) adamw_norm_kernel(const __grid_constant__
         }
       }
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u) {  // eight squares in fp32, the rest in fp64
+        float sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum[u] += x[u][j] * x[u][j];
+        for (int j = 0; j < 8; ++j) sum += x[u][j] * x[u][j];
+        s += (double)sum;
+      }
     }
-    s = (double)sum[0] + (double)sum[1];
     const long long edge = t < 8 ? f0 + t : (a1 > a0 ? a1 : a0) + t - 8;  // elements before the first and behind the last vector
     if (t < 16 && edge < f1 && (t >= 8 || edge < a0)) {
       const float x = load1(G, GDT, edge);
-      s += (double)(x * x);
+      s += (double)x * (double)x;
     }
   } else if (q == tab.start[i]) {  // its first chunk stands for the whole tensor
     const int count = *T.rowsq_count;
@@ -147,7 +151,7 @@ __global__ void __launch_bounds__(256) adamw_norm_kernel(const __grid_constant__
   for (unsigned x = t; x < many; x += 256) a += __ldcg(p + x);
   const double total = block_sum(a, red[1]);
   if (t == 0 && !isfinite(total)) atomicOr(c.status, LORDO_FLAG_NONFINITE_GRAD);
-  const float coef = fminf(1.f, c.rho / ((float)sqrt(total) + 1e-6f));
+  const float coef = (float)fmin(1.0, c.rho / (sqrt(total) + 1e-6));
   if (c.scope) {
     if (t == 0) c.coef[(long long)index * l.K + k] = coef;
   } else {
@@ -158,10 +162,15 @@ __global__ void __launch_bounds__(256) adamw_norm_kernel(const __grid_constant__
 // ---------------------------------------------------------------------------------------------
 // Step, 32-bit moments
 // ---------------------------------------------------------------------------------------------
+// The moments' operations are rounded one by one, as written in the definition: what a compiler fuses must not decide how 8-bit codes round.
+__device__ __forceinline__ void moments(const AwStep& s, float g, float& m, float& v) {
+  m = __fadd_rn(__fmul_rn(s.b1, m), __fmul_rn(s.a1, g));
+  v = __fadd_rn(__fmul_rn(s.b2, v), __fmul_rn(__fmul_rn(s.a2, g), g));
+}
+
 __device__ __forceinline__ void update(const AwStep& s, float wd, float c, float g, float& m, float& v, float& w) {
-  g *= c;
-  m = s.b1 * m + s.a1 * g;
-  v = s.b2 * v + s.a2 * g * g;
+  g = __fmul_rn(g, c);
+  moments(s, g, m, v);
   const float up = (s.omega * (m * s.inv_bc1) + s.a_omega * g) / (sqrtf(v * s.inv_bc2) + s.eps);
   w -= s.lr * (up + wd * w);
 }
@@ -221,19 +230,156 @@ __device__ __forceinline__ int scale_code(unsigned top) {
 }
 __device__ __forceinline__ float pow2(int code) { return __int_as_float(code << 23); }  // 2^(code - 127), code in [1, 254]
 
-// E4M3 code of a magnitude t < 256, rounded down after (u + 1/2) / 65536 of a step was added. Below 2^-6 the steps are 2^-9 wide, as they
-// are for t + 2^-6. Infinities and NaN become NaN.
-__device__ __forceinline__ int code8(float t, unsigned u) {
+// E4M3 code of a magnitude t < 256, rounded down after (u + 1/2) / 65536 of a step was added; u16 = 16 u. Below 2^-6 the steps are 2^-9
+// wide, as they are for t + 2^-6. Infinities and NaN become NaN.
+__device__ __forceinline__ unsigned code8(float t, unsigned u16) {
   const bool sub = t < 0.015625f;
   const unsigned b = __float_as_uint(fabsf(sub ? t + 0.015625f : t));
-  const int code = (int)((b + (u << 4) + 8u) >> 20) - (sub ? 968 : 960);
-  return code > 127 ? 127 : code;
+  const int code = (int)((b + u16 + 8u) >> 20) - (sub ? 968 : 960);
+  return (unsigned)(code > 127 ? 127 : code);
 }
-__device__ __forceinline__ float value8(unsigned byte) {  // of an E4M3 code
-  const unsigned e = byte & 0x7Fu;
-  float x = __uint_as_float((e << 20)) * __uint_as_float(0x7B800000u);  // 2^120: moves the exponent's bias, subnormals too
-  if (e == 127u) x = __uint_as_float(0x7FC00000u);
-  return byte & 0x80u ? -x : x;
+// The same for finite t in [2^-6, 256), in the top seven bits behind the sign's place.
+__device__ __forceinline__ unsigned code8_normal(float t, unsigned u16) { return (__float_as_uint(t) + u16 + (8u - (960u << 20))) << 4; }
+
+// Four values of E4M3 codes.
+__device__ __forceinline__ void values8(unsigned c, float* x) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(c >> (16 * h)), __NV_E4M3);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r));
+    x[2 * h] = f.x;
+    x[2 * h + 1] = f.y;
+  }
+}
+
+// 16 times the 16 random bits of element j of four, for the first moment and for the second
+__device__ __forceinline__ unsigned first16(unsigned long long r, int j) {
+  const unsigned w = j < 2 ? (unsigned)r : (unsigned)(r >> 32);
+  return (j & 1 ? w >> 12 : w << 4) & 0xFFFF0u;
+}
+__device__ __forceinline__ unsigned second16(unsigned first) { return (first * 40503u) & 0xFFFF0u; }
+
+constexpr unsigned kInfBits = 0x7F800000u;
+
+__device__ __forceinline__ unsigned top8(const float (&x)[8]) {
+  unsigned t = 0u;
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) t = __vimax3_u32(t, __float_as_uint(x[j]) & 0x7FFFFFFFu, __float_as_uint(x[j + 1]) & 0x7FFFFFFFu);
+  return t;
+}
+__device__ __forceinline__ unsigned low8(const float (&x)[8]) {
+  unsigned t = 0xFFFFFFFFu;
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) t = __vimin3_u32(t, __float_as_uint(x[j]) & 0x7FFFFFFFu, __float_as_uint(x[j + 1]) & 0x7FFFFFFFu);
+  return t;
+}
+
+// Codes of four elements. NORMAL: every |x| inv lies in [2^-6, 256).
+template <bool SECOND, bool NORMAL>
+__device__ __forceinline__ unsigned pack8(const float* x, float inv, const unsigned (&u16)[4]) {
+  unsigned b[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const unsigned u = SECOND ? second16(u16[j]) : u16[j];
+    const unsigned bits = __float_as_uint(x[j]);
+    if (NORMAL) {
+      b[j] = code8_normal(fabsf(x[j]) * inv, u);
+    } else {
+      unsigned c = code8(fabsf(x[j]) * inv, u);
+      if (SECOND && c == 0u && x[j] > 0.f) c = 1u;
+      b[j] = c << 24;
+    }
+    b[j] = SECOND ? b[j] : (b[j] & 0x7FFFFFFFu) | (bits & 0x80000000u);
+  }
+  return __byte_perm(__byte_perm(b[0], b[1], 0x0073), __byte_perm(b[2], b[3], 0x0073), 0x5410);  // the top byte of each
+}
+
+// A block of 256 elements of one worker's tensor, a lane has eight.
+template <int WDT, int GDT>
+__device__ __forceinline__ void step8_block(const AwTensor& T, const void* G, const AwStep& s, float c, unsigned long long key, int k, long long base, long long b,
+                                            int lane) {
+  unsigned char* M = reinterpret_cast<unsigned char*>(T.m);
+  unsigned char* V = reinterpret_cast<unsigned char*>(T.v);
+  const long long e = b * kAwBlock + 8 * lane, f = base + e;
+  const bool vec = ((base & 7) == 0) && e + 8 <= T.n;
+  const int left = e >= T.n ? 0 : T.n - e < 8 ? (int)(T.n - e) : 8;
+  float g[8], w[8], m[8], r[8];
+  unsigned mc[2] = {0u, 0u}, vc[2] = {0u, 0u};
+  if (vec) {
+    if (G) load8<GDT>(G, f, g); else row_grad8(T, k, e, g);
+    load8<WDT>(T.W, f, w);
+    const uint2 a = *reinterpret_cast<const uint2*>(M + f), d = *reinterpret_cast<const uint2*>(V + f);
+    mc[0] = a.x; mc[1] = a.y; vc[0] = d.x; vc[1] = d.y;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      g[j] = w[j] = 0.f;
+      if (j < left) {
+        g[j] = G ? load1(G, GDT, f + j) : row_grad(T, k, e + j);
+        w[j] = load1(T.W, WDT, f + j);
+        mc[j >> 2] |= (unsigned)M[f + j] << (8 * (j & 3));
+        vc[j >> 2] |= (unsigned)V[f + j] << (8 * (j & 3));
+      }
+    }
+  }
+  const long long sb = (long long)k * T.nb + b;
+  const float ms = pow2(T.ms[sb]), vs = pow2(T.vs[sb]);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    values8(mc[h], m + 4 * h);
+    values8(vc[h], r + 4 * h);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    g[j] = __fmul_rn(g[j], c);
+    m[j] *= ms;
+    r[j] *= vs;
+    float v = r[j] * r[j];
+    moments(s, g[j], m[j], v);
+    r[j] = sqrtf(v);
+    // the quotient is not kept: two units in its last place are enough
+    const float up = __fdividef(s.omega * (m[j] * s.inv_bc1) + s.a_omega * g[j], r[j] * s.root_inv_bc2 + s.eps);
+    w[j] -= s.lr * (up + T.wd * w[j]);
+  }
+  const unsigned mtop = __reduce_max_sync(0xffffffffu, top8(m)), vtop = __reduce_max_sync(0xffffffffu, top8(r));
+  const int mcode = scale_code(mtop), vcode = scale_code(vtop);
+  const float mi = pow2(254 - mcode), vi = pow2(254 - vcode);
+  // magnitudes below 2^-6 of the grid, which take half as many instructions again, are rare: a block has them or it has not
+  const bool low = __uint_as_float(low8(m)) * mi < 0.015625f || __uint_as_float(low8(r)) * vi < 0.015625f;
+  const bool slow = __any_sync(0xffffffffu, low) || mtop >= kInfBits || vtop >= kInfBits;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const unsigned long long x = bits4(key, e + 4 * h);
+    unsigned u[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[j] = first16(x, j);
+    if (slow) {
+      mc[h] = pack8<false, false>(m + 4 * h, mi, u);
+      vc[h] = pack8<true, false>(r + 4 * h, vi, u);
+    } else {
+      mc[h] = pack8<false, true>(m + 4 * h, mi, u);
+      vc[h] = pack8<true, true>(r + 4 * h, vi, u);
+    }
+  }
+  if (vec) {
+    store8<WDT>(T.W, f, w);
+    *reinterpret_cast<uint2*>(M + f) = make_uint2(mc[0], mc[1]);
+    *reinterpret_cast<uint2*>(V + f) = make_uint2(vc[0], vc[1]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (j < left) {
+        store1(T.W, WDT, f + j, w[j]);
+        M[f + j] = (unsigned char)(mc[j >> 2] >> (8 * (j & 3)));
+        V[f + j] = (unsigned char)(vc[j >> 2] >> (8 * (j & 3)));
+      }
+    }
+  }
+  // every lane has read the scales before the reductions above
+  if (lane == 0) {
+    T.ms[sb] = (unsigned char)mcode;
+    T.vs[sb] = (unsigned char)vcode;
+  }
 }
 
 template <int WDT, int GDT>
@@ -248,90 +394,15 @@ __global__ void __launch_bounds__(256) adamw_step8_kernel(const __grid_constant_
   dep_begin();
   const float c = coef ? __ldcg(coef + (long long)T.index * stride + k) : 1.f;
   const long long base = (long long)k * T.n;
-  unsigned char* M = reinterpret_cast<unsigned char*>(T.m);
-  unsigned char* V = reinterpret_cast<unsigned char*>(T.v);
   const long long b0 = (long long)(q - tab.start[i]) * (kAwPiece / kAwBlock);
-  for (int x = warp; x < kAwPiece / kAwBlock; x += 8) {
-    const long long b = b0 + x;
-    if (b >= T.nb) break;
-    const long long e = b * kAwBlock + 8 * lane, f = base + e;
-    const bool vec = ((base & 7) == 0) && e + 8 <= T.n;
-    const int left = e >= T.n ? 0 : T.n - e < 8 ? (int)(T.n - e) : 8;
-    float g[8], w[8], m[8], v[8];
-    unsigned mc[2] = {0u, 0u}, vc[2] = {0u, 0u};
-    if (vec) {
-      if (G) load8<GDT>(G, f, g); else row_grad8(T, k, e, g);
-      load8<WDT>(T.W, f, w);
-      const uint2 a = *reinterpret_cast<const uint2*>(M + f), d = *reinterpret_cast<const uint2*>(V + f);
-      mc[0] = a.x; mc[1] = a.y; vc[0] = d.x; vc[1] = d.y;
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        g[j] = w[j] = 0.f;
-        if (j < left) {
-          g[j] = G ? load1(G, GDT, f + j) : row_grad(T, k, e + j);
-          w[j] = load1(T.W, WDT, f + j);
-          mc[j >> 2] |= (unsigned)M[f + j] << (8 * (j & 3));
-          vc[j >> 2] |= (unsigned)V[f + j] << (8 * (j & 3));
-        }
-      }
-    }
-    const long long sb = (long long)k * T.nb + b;
-    const float ms = pow2(T.ms[sb]), vs = pow2(T.vs[sb]);
-    unsigned mtop = 0u, vtop = 0u;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      m[j] = value8((mc[j >> 2] >> (8 * (j & 3))) & 0xFFu) * ms;
-      const float r = value8((vc[j >> 2] >> (8 * (j & 3))) & 0xFFu) * vs;
-      v[j] = r * r;
-      update(s, T.wd, c, g[j], m[j], v[j], w[j]);
-      v[j] = sqrtf(v[j]);
-      const unsigned ma = __float_as_uint(m[j]) & 0x7FFFFFFFu, va = __float_as_uint(v[j]);
-      mtop = ma > mtop ? ma : mtop;
-      vtop = va > vtop ? va : vtop;
-    }
-    const int mcode = scale_code(__reduce_max_sync(0xffffffffu, mtop)), vcode = scale_code(__reduce_max_sync(0xffffffffu, vtop));
-    const float mi = pow2(254 - mcode), vi = pow2(254 - vcode);
-    mc[0] = mc[1] = vc[0] = vc[1] = 0u;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const unsigned long long r = bits4(key, e + 4 * h);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const unsigned u = (unsigned)(r >> (16 * j)) & 0xFFFFu;
-        const float x = m[4 * h + j], y = v[4 * h + j];
-        const unsigned a = (unsigned)code8(fabsf(x) * mi, u) | ((__float_as_uint(x) >> 24) & 0x80u);
-        unsigned d = (unsigned)code8(y * vi, (u * 40503u) & 0xFFFFu);
-        if (d == 0u && y > 0.f) d = 1u;
-        mc[h] |= a << (8 * j);
-        vc[h] |= d << (8 * j);
-      }
-    }
-    if (vec) {
-      store8<WDT>(T.W, f, w);
-      *reinterpret_cast<uint2*>(M + f) = make_uint2(mc[0], mc[1]);
-      *reinterpret_cast<uint2*>(V + f) = make_uint2(vc[0], vc[1]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (j < left) {
-          store1(T.W, WDT, f + j, w[j]);
-          M[f + j] = (unsigned char)(mc[j >> 2] >> (8 * (j & 3)));
-          V[f + j] = (unsigned char)(vc[j >> 2] >> (8 * (j & 3)));
-        }
-      }
-    }
-    __syncwarp();  // every lane has read the scales
-    if (lane == 0) {
-      T.ms[sb] = (unsigned char)mcode;
-      T.vs[sb] = (unsigned char)vcode;
-    }
-  }
+  const long long b1 = b0 + kAwPiece / kAwBlock < T.nb ? b0 + kAwPiece / kAwBlock : T.nb;
+  for (long long b = b0 + warp; b < b1; b += 8) step8_block<WDT, GDT>(T, G, s, c, key, k, base, b, lane);
 }
 
 // ---------------------------------------------------------------------------------------------
 // Outer synchronisation: moments <- mean over the workers; D = X0 - mean W; average: X0 <- X0 - D; Nesterov: B <- mu B + D,
-// X0 <- X0 - eta (D + mu B); every W_k <- X0.
+// X0 <- X0 - eta (D + mu B); every W_k <- X0. Each operation is rounded on its own: with bf16 weights D of the next synchronisation is
+// what X0 loses in its cast, and a last bit that depends on what a compiler fuses would become a whole step of bf16 there.
 // ---------------------------------------------------------------------------------------------
 template <int WDT, int N>  // N consecutive elements of every worker: 4 (a float4's alignment everywhere) or 1
 __device__ __forceinline__ void outer_weights(const AwTensor& T, int K, const AwOuter& o, float inv_k, long long e) {
@@ -348,10 +419,10 @@ __device__ __forceinline__ void outer_weights(const AwTensor& T, int K, const Aw
 #pragma unroll
   for (int j = 0; j < N; ++j) {
     x0[j] = T.X0[e + j];
-    const float d = x0[j] - s[j] * inv_k;
+    const float d = __fsub_rn(x0[j], __fmul_rn(s[j], inv_k));
     if (o.nesterov) {
-      b[j] = o.mu * T.B[e + j] + d;
-      x0[j] -= o.eta * (d + o.mu * b[j]);
+      b[j] = __fadd_rn(__fmul_rn(o.mu, T.B[e + j]), d);
+      x0[j] = __fsub_rn(x0[j], __fmul_rn(o.eta, __fadd_rn(d, __fmul_rn(o.mu, b[j]))));
     } else {
       x0[j] -= d;
     }
@@ -431,36 +502,28 @@ __device__ __forceinline__ void outer_mean8(const AwTensor& T, int K, float inv_
       for (int j = 0; j < 8; ++j)
         if (j < left) c[j >> 2] |= (unsigned)p[j] << (8 * (j & 3));
     }
+    float x[8];
+    values8(c[0], x);
+    values8(c[1], x + 4);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float x = value8((c[j >> 2] >> (8 * (j & 3))) & 0xFFu) * scale;
-      a[j] += SECOND ? x * x : x;
+      x[j] *= scale;
+      a[j] += SECOND ? x[j] * x[j] : x[j];
     }
   }
-  unsigned top = 0u;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     a[j] *= inv_k;
     if (SECOND) a[j] = sqrtf(a[j]);
-    const unsigned x = __float_as_uint(a[j]) & 0x7FFFFFFFu;
-    top = x > top ? x : top;
   }
-  const int code = scale_code(__reduce_max_sync(0xffffffffu, top));
+  const int code = scale_code(__reduce_max_sync(0xffffffffu, top8(a)));
   const float inv = pow2(254 - code);
-  unsigned c[2] = {0u, 0u};
+  unsigned c[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const unsigned long long r = bits4(key, e + 4 * h);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      unsigned u = (unsigned)(r >> (16 * j)) & 0xFFFFu;
-      if (SECOND) u = (u * 40503u) & 0xFFFFu;
-      const float x = a[4 * h + j];
-      unsigned y = (unsigned)code8(fabsf(x) * inv, u);
-      if (SECOND) { if (y == 0u && x > 0.f) y = 1u; }
-      else y |= (__float_as_uint(x) >> 24) & 0x80u;
-      c[h] |= y << (8 * j);
-    }
+    const unsigned u[4] = {first16(r, 0), first16(r, 1), first16(r, 2), first16(r, 3)};
+    c[h] = pack8<SECOND, false>(a + 4 * h, inv, u);
   }
   for (int k = 0; k < K; ++k) {
     unsigned char* p = C + (long long)k * T.n + e;

@@ -36,7 +36,7 @@ struct AwTable {
 struct AwStep {
   float lr, b1, a1, b2, a2;  // a = 1 - b
   float omega, a_omega, eps;
-  float inv_bc1, inv_bc2;
+  float inv_bc1, inv_bc2, root_inv_bc2;
   unsigned long long key;    // of the rounding, for this step
 };
 
@@ -52,7 +52,7 @@ struct AwClip {
   double* partial;     // [K][total]
   unsigned total, at;  // chunks of a worker in all launches, and before this one
   unsigned* tickets;   // scope 0: [K]; scope 1: [n_tensors][K]; zero before the first launch, and again after every step
-  float rho;
+  double rho;
   int scope, n_tensors;
   float* coef;         // [n_tensors][K]
   unsigned* status;

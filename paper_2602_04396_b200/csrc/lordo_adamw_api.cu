@@ -62,13 +62,13 @@ int validate(const lordo_adamw_config* cfg) {
   auto dt_ok = [](int d) { return d == LORDO_F32 || d == LORDO_BF16; };
   if (!dt_ok(cfg->w_dtype) || !dt_ok(cfg->g_dtype)) return LORDO_ERR_INVALID_ARG;
   if (cfg->states != LORDO_STATES_F32 && cfg->states != LORDO_STATES_8BIT) return LORDO_ERR_INVALID_ARG;
-  if (!(cfg->beta2 >= 0.f && cfg->beta2 < 1.f) || !(cfg->eps > 0.f)) return LORDO_ERR_INVALID_ARG;
+  if (!(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) || !((float)cfg->eps > 0.f)) return LORDO_ERR_INVALID_ARG;
   if (cfg->clip_scope != 0 && cfg->clip_scope != 1) return LORDO_ERR_INVALID_ARG;
   if (cfg->outer != LORDO_OUTER_AVG && cfg->outer != LORDO_OUTER_NESTEROV) return LORDO_ERR_INVALID_ARG;
   long long elements = 0;
   for (int i = 0; i < cfg->n_tensors; ++i) {
     const lordo_tensor& t = cfg->tensors[i];
-    if (t.n < 1 || t.row < 0 || t.max_tokens < 0 || t.pad != 0) return LORDO_ERR_SHAPE;
+    if (t.n < 1 || t.row < 0 || t.max_tokens < 0) return LORDO_ERR_SHAPE;
     if (!std::isfinite(t.weight_decay)) return LORDO_ERR_INVALID_ARG;
     if (t.n > (1ll << 40)) return LORDO_ERR_UNSUPPORTED;
     if (t.row == 0 && t.max_tokens != 0) return LORDO_ERR_SHAPE;
@@ -127,7 +127,7 @@ size_t build(lordo_adamw_ctx* c, const lordo_adamw_buffers* buf, char* base) {
   for (int i = 0; i < nt; ++i) {
     const lordo_tensor& t = cfg.tensors[i];
     AwTensor& a = c->h_tensors[i];
-    a.n = t.n; a.nb = cdiv(t.n, kAwBlock); a.wd = t.weight_decay; a.index = i; a.d = t.row; a.cap = t.max_tokens;
+    a.n = t.n; a.nb = cdiv(t.n, kAwBlock); a.wd = (float)t.weight_decay; a.index = i; a.d = t.row; a.cap = t.max_tokens;
     if (buf) {
       a.W = buf->W[i]; a.m = buf->m[i]; a.v = buf->v[i];
       if (cfg.states == LORDO_STATES_8BIT) {
@@ -176,7 +176,7 @@ int refuse_capture(lordo_adamw_ctx* c, cudaStream_t st) {
   return LORDO_OK;
 }
 
-int step(lordo_adamw_ctx* c, const lordo_grad* G, float lr, float beta1, float omega, const float* coef_dev, cudaStream_t st) {
+int step(lordo_adamw_ctx* c, const lordo_grad* G, double lr, double beta1, double omega, const float* coef_dev, cudaStream_t st) {
   const lordo_adamw_config& cfg = c->cfg;
   for (int i = 0; i < cfg.n_tensors; ++i) {
     const lordo_grad& g = G[i];
@@ -210,7 +210,7 @@ int step(lordo_adamw_ctx* c, const lordo_grad* G, float lr, float beta1, float o
   }
   const float* coef = coef_dev;
   int stride = 0;
-  if (!coef && cfg.clip_rho > 0.f) {
+  if (!coef && cfg.clip_rho > 0.0) {
     for (Group& g : c->groups) {
       const AwClip clip = {c->d_partial, c->total_chunks, g.chunks_before, c->d_tickets, cfg.clip_rho, cfg.clip_scope, cfg.n_tensors, c->d_coef, c->d_status};
       launch_aw_norm(launch_of(c, g, g.chunks), g.norm, clip, st);
@@ -221,10 +221,11 @@ int step(lordo_adamw_ctx* c, const lordo_grad* G, float lr, float beta1, float o
   }
   const int64_t s = c->steps + 1;
   AwStep a;
-  a.lr = lr; a.b1 = beta1; a.a1 = (float)(1.0 - (double)beta1); a.b2 = cfg.beta2; a.a2 = (float)(1.0 - (double)cfg.beta2);
-  a.omega = omega; a.a_omega = (float)(1.0 - (double)omega); a.eps = cfg.eps;
-  a.inv_bc1 = (float)(1.0 / (1.0 - std::pow((double)beta1, (double)s)));
-  a.inv_bc2 = (float)(1.0 / (1.0 - std::pow((double)cfg.beta2, (double)s)));
+  a.lr = (float)lr; a.b1 = (float)beta1; a.a1 = (float)(1.0 - beta1); a.b2 = (float)cfg.beta2; a.a2 = (float)(1.0 - cfg.beta2);
+  a.omega = (float)omega; a.a_omega = (float)(1.0 - omega); a.eps = (float)cfg.eps;
+  a.inv_bc1 = (float)(1.0 / (1.0 - std::pow(beta1, (double)s)));
+  a.inv_bc2 = (float)(1.0 / (1.0 - std::pow(cfg.beta2, (double)s)));
+  a.root_inv_bc2 = (float)std::sqrt(1.0 / (1.0 - std::pow(cfg.beta2, (double)s)));
   a.key = stream_key(cfg.seed, 3, 0, s, 0);
   for (Group& g : c->groups) {
     launch_aw_step(launch_of(c, g, g.pieces), g.step, coef, stride, a, st);
@@ -306,10 +307,10 @@ int lordo_adamw_init(const lordo_adamw_config* cfg, const lordo_adamw_buffers* b
   return LORDO_OK;
 }
 
-int lordo_adamw_step(lordo_adamw_ctx* c, const lordo_grad* G, float lr, float beta1, float omega, const float* coef_dev, void* stream) {
+int lordo_adamw_step(lordo_adamw_ctx* c, const lordo_grad* G, double lr, double beta1, double omega, const float* coef_dev, void* stream) {
   if (!c) return LORDO_ERR_INVALID_ARG;
   if (!G) return fail(c, LORDO_ERR_INVALID_ARG, "G is null");
-  if (!(beta1 >= 0.f && beta1 < 1.f) || !(omega >= 0.f && omega <= 1.f)) return fail(c, LORDO_ERR_INVALID_ARG, "beta1 or omega out of range");
+  if (!(beta1 >= 0.0 && beta1 < 1.0) || !(omega >= 0.0 && omega <= 1.0)) return fail(c, LORDO_ERR_INVALID_ARG, "beta1 or omega out of range");
   return step(c, G, lr, beta1, omega, coef_dev, reinterpret_cast<cudaStream_t>(stream));
 }
 
@@ -321,7 +322,7 @@ int lordo_adamw_outer_step(lordo_adamw_ctx* c, void* stream) {
   if (rc != LORDO_OK) return rc;
   rc = check_launch(c, "before the synchronisation");
   if (rc != LORDO_OK) return rc;
-  const AwOuter o = {c->cfg.sync_m, c->cfg.sync_v, c->cfg.outer == LORDO_OUTER_NESTEROV, c->cfg.outer_lr, c->cfg.outer_momentum,
+  const AwOuter o = {c->cfg.sync_m, c->cfg.sync_v, c->cfg.outer == LORDO_OUTER_NESTEROV, (float)c->cfg.outer_lr, (float)c->cfg.outer_momentum,
                      stream_key(c->cfg.seed, 4, 0, c->outers, 0)};
   for (Group& g : c->groups) {
     launch_aw_outer(launch_of(c, g, g.blocks), g.d_outer, o, st);

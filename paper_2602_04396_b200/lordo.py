@@ -58,15 +58,15 @@ class _Buffers(C.Structure):
 
 
 class _Tensor(C.Structure):
-    _fields_ = [("n", C.c_int64), ("row", C.c_int64), ("max_tokens", C.c_int64), ("weight_decay", C.c_float), ("pad", C.c_int32)]
+    _fields_ = [("n", C.c_int64), ("row", C.c_int64), ("max_tokens", C.c_int64), ("weight_decay", C.c_double)]
 
 
 class _AdamWConfig(C.Structure):
     _fields_ = [
         ("n_tensors", C.c_int32), ("tensors", C.POINTER(_Tensor)), ("K", C.c_int32), ("w_dtype", C.c_int32), ("g_dtype", C.c_int32),
-        ("states", C.c_int32), ("beta2", C.c_float), ("eps", C.c_float), ("clip_rho", C.c_float), ("clip_scope", C.c_int32),
-        ("sync", C.c_int32), ("sync_m", C.c_int32), ("sync_v", C.c_int32), ("outer", C.c_int32), ("outer_lr", C.c_float),
-        ("outer_momentum", C.c_float), ("seed", C.c_uint64),
+        ("states", C.c_int32), ("beta2", C.c_double), ("eps", C.c_double), ("clip_rho", C.c_double), ("clip_scope", C.c_int32),
+        ("sync", C.c_int32), ("sync_m", C.c_int32), ("sync_v", C.c_int32), ("outer", C.c_int32), ("outer_lr", C.c_double),
+        ("outer_momentum", C.c_double), ("seed", C.c_uint64),
     ]
 
 
@@ -122,7 +122,7 @@ def load_library() -> C.CDLL:
     lib.lordo_embedding_grad.argtypes = [vp, i32, vp, i32, i32, i64, i64, i64, f32, vp, i32, i32, vp, C.c_size_t, vp]
     lib.lordo_adamw_query_workspace.argtypes = [C.POINTER(_AdamWConfig), C.POINTER(C.c_size_t)]
     lib.lordo_adamw_init.argtypes = [C.POINTER(_AdamWConfig), C.POINTER(_AdamWBuffers), vp, C.c_size_t, vp, C.POINTER(vp)]
-    lib.lordo_adamw_step.argtypes = [vp, C.POINTER(_Grad), f32, f32, f32, vp, vp]
+    lib.lordo_adamw_step.argtypes = [vp, C.POINTER(_Grad), C.c_double, C.c_double, C.c_double, vp, vp]
     lib.lordo_adamw_outer_step.argtypes = [vp, vp]
     lib.lordo_adamw_poll_status.argtypes = [vp, vp, C.POINTER(C.c_uint32)]
     lib.lordo_adamw_clear_status.argtypes = [vp, vp]
