@@ -185,8 +185,8 @@ __global__ void __launch_bounds__(256) adamw_step_kernel(const __grid_constant__
   const void* G = tab.G[i];
   dep_begin();
   const float c = coef ? __ldcg(coef + (long long)T.index * stride + k) : 1.f;
-  const long long e0 = (long long)(q - tab.start[i]) * kAwPiece;
-  const long long e1 = e0 + kAwPiece < T.n ? e0 + kAwPiece : T.n;
+  const long long e0 = (long long)(q - tab.start[i]) * l.piece;
+  const long long e1 = e0 + l.piece < T.n ? e0 + l.piece : T.n;
   const long long base = (long long)k * T.n, f0 = base + e0, f1 = base + e1;
   const long long a0 = (f0 + 7) & ~7ll, a1 = f1 & ~7ll;
   float* M = reinterpret_cast<float*>(T.m);
@@ -220,8 +220,8 @@ __global__ void __launch_bounds__(256) adamw_step_kernel(const __grid_constant__
 // of two for scales a value stays where it is on the grid when the largest of its block changes; an fp32 scale (the largest itself) would
 // move all 256 off the grid in every step, and the noise of rounding them again would add up. sqrt(v) has half the range of v.
 // ---------------------------------------------------------------------------------------------
-// 16 random bits for each of four consecutive elements
-__device__ __forceinline__ unsigned long long bits4(unsigned long long key, long long e) { return mix64(key + kGolden * (unsigned long long)((e >> 2) + 1)); }
+// What the generator mixes to 16 random bits for each of four consecutive elements; the next four are kGolden on.
+__device__ __forceinline__ unsigned long long counter4(unsigned long long key, long long e) { return key + kGolden * (unsigned long long)((e >> 2) + 1); }
 
 // Exponent byte of the scale that puts `top` (the bits of a magnitude) into [128, 256) times itself.
 __device__ __forceinline__ int scale_code(unsigned top) {
@@ -294,36 +294,32 @@ __device__ __forceinline__ unsigned pack8(const float* x, float inv, const unsig
   return __byte_perm(__byte_perm(b[0], b[1], 0x0073), __byte_perm(b[2], b[3], 0x0073), 0x5410);  // the top byte of each
 }
 
-// A block of 256 elements of one worker's tensor, a lane has eight.
-template <int WDT, int GDT>
-__device__ __forceinline__ void step8_block(const AwTensor& T, const void* G, const AwStep& s, float c, unsigned long long key, int k, long long base, long long b,
-                                            int lane) {
-  unsigned char* M = reinterpret_cast<unsigned char*>(T.m);
-  unsigned char* V = reinterpret_cast<unsigned char*>(T.v);
-  const long long e = b * kAwBlock + 8 * lane, f = base + e;
-  const bool vec = ((base & 7) == 0) && e + 8 <= T.n;
-  const int left = e >= T.n ? 0 : T.n - e < 8 ? (int)(T.n - e) : 8;
-  float g[8], w[8], m[8], r[8];
-  unsigned mc[2] = {0u, 0u}, vc[2] = {0u, 0u};
-  if (vec) {
-    if (G) load8<GDT>(G, f, g); else row_grad8(T, k, e, g);
-    load8<WDT>(T.W, f, w);
-    const uint2 a = *reinterpret_cast<const uint2*>(M + f), d = *reinterpret_cast<const uint2*>(V + f);
-    mc[0] = a.x; mc[1] = a.y; vc[0] = d.x; vc[1] = d.y;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      g[j] = w[j] = 0.f;
-      if (j < left) {
-        g[j] = G ? load1(G, GDT, f + j) : row_grad(T, k, e + j);
-        w[j] = load1(T.W, WDT, f + j);
-        mc[j >> 2] |= (unsigned)M[f + j] << (8 * (j & 3));
-        vc[j >> 2] |= (unsigned)V[f + j] << (8 * (j & 3));
-      }
-    }
-  }
-  const long long sb = (long long)k * T.nb + b;
-  const float ms = pow2(T.ms[sb]), vs = pow2(T.vs[sb]);
+// sqrt(v) by one of Newton's (Heron's) steps on r^2 = v from r = v rsqrt(v), whose derivative 2 r is 2 / rsqrt(v): of normal numbers off by less than
+// a unit in the last place, as a rule rounded to the nearest. The step is not a number for 0 (and below 2^-126), infinity and NaN; the maximum
+// then takes v 1e-20, which is 0, infinity and NaN, and below the root of any other v. Seven instructions without a branch; sqrtf has one.
+__device__ __forceinline__ float root(float v) {
+  float y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(v));
+  const float r = v * y;
+  return fmaxf(fmaf(fmaf(-r, r, v), 0.5f * y, r), v * 1e-20f);
+}
+__device__ __forceinline__ float reciprocal(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+struct Step8 {  // constants of a step, of its worker and tensor
+  float c, b1, a1, b2, a2, keep, lm, lg, root_inv_bc2, eps;
+};
+
+// A lane's eight elements of a block of 256 of one worker's tensor: codes in, codes and scales out. The scales are powers of two, so that b1 (m8 S) is
+// (b1 S) m8 to the last bit, and b2 (s8 S)^2 is (b2 S^2) s8^2.
+__device__ __forceinline__ void step8_lane(const Step8& s, unsigned long long counter, float (&g)[8], float (&w)[8], unsigned (&mc)[2], unsigned (&vc)[2],
+                                           int& mcode, int& vcode) {
+  const float ms = pow2(mcode), vs = pow2(vcode);
+  const float b1 = s.b1 * ms, b2 = s.b2 * (vs * vs);
+  float m[8], r[8];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     values8(mc[h], m + 4 * h);
@@ -331,25 +327,21 @@ __device__ __forceinline__ void step8_block(const AwTensor& T, const void* G, co
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    g[j] = __fmul_rn(g[j], c);
-    m[j] *= ms;
-    r[j] *= vs;
-    float v = r[j] * r[j];
-    moments(s, g[j], m[j], v);
-    r[j] = sqrtf(v);
-    // the quotient is not kept: two units in its last place are enough
-    const float up = __fdividef(s.omega * (m[j] * s.inv_bc1) + s.a_omega * g[j], r[j] * s.root_inv_bc2 + s.eps);
-    w[j] -= s.lr * (up + T.wd * w[j]);
+    const float x = __fmul_rn(g[j], s.c);
+    m[j] = __fadd_rn(__fmul_rn(b1, m[j]), __fmul_rn(s.a1, x));
+    r[j] = root(__fadd_rn(__fmul_rn(b2, r[j] * r[j]), __fmul_rn(__fmul_rn(s.a2, x), x)));
+    w[j] = fmaf(-(s.lm * m[j] + s.lg * x), reciprocal(fmaf(r[j], s.root_inv_bc2, s.eps)), w[j] * s.keep);
   }
   const unsigned mtop = __reduce_max_sync(0xffffffffu, top8(m)), vtop = __reduce_max_sync(0xffffffffu, top8(r));
-  const int mcode = scale_code(mtop), vcode = scale_code(vtop);
+  mcode = scale_code(mtop);
+  vcode = scale_code(vtop);
   const float mi = pow2(254 - mcode), vi = pow2(254 - vcode);
   // magnitudes below 2^-6 of the grid, which take half as many instructions again, are rare: a block has them or it has not
   const bool low = __uint_as_float(low8(m)) * mi < 0.015625f || __uint_as_float(low8(r)) * vi < 0.015625f;
   const bool slow = __any_sync(0xffffffffu, low) || mtop >= kInfBits || vtop >= kInfBits;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const unsigned long long x = bits4(key, e + 4 * h);
+    const unsigned long long x = mix64(counter + h * kGolden);
     unsigned u[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) u[j] = first16(x, j);
@@ -361,42 +353,170 @@ __device__ __forceinline__ void step8_block(const AwTensor& T, const void* G, co
       vc[h] = pack8<true, true>(r + 4 * h, vi, u);
     }
   }
-  if (vec) {
-    store8<WDT>(T.W, f, w);
-    *reinterpret_cast<uint2*>(M + f) = make_uint2(mc[0], mc[1]);
-    *reinterpret_cast<uint2*>(V + f) = make_uint2(vc[0], vc[1]);
+}
+
+struct Arrays8 {  // of one worker
+  const void* G;
+  void* W;
+  unsigned char *m, *v, *ms, *vs;
+};
+
+template <int BYTES>
+__device__ __forceinline__ void copy_async(unsigned to, const void* from) {
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
+}
+template <int DT>
+__device__ __forceinline__ void copy8(unsigned to, const void* base, long long at) {  // eight elements, 32 lanes' 16 bytes side by side
+  const char* p = reinterpret_cast<const char*>(base) + at * (DT == LORDO_F32 ? 4 : 2);
+  copy_async<16>(to, p);
+  if constexpr (DT == LORDO_F32) copy_async<16>(to + 512, p + 16);
+}
+template <int DT>
+__device__ __forceinline__ void shared8(const char* from, float (&x)[8]) {
+  const uint4 a = *reinterpret_cast<const uint4*>(from);
+  if constexpr (DT == LORDO_F32) {
+    const uint4 b = *reinterpret_cast<const uint4*>(from + 512);
+    x[0] = __uint_as_float(a.x); x[1] = __uint_as_float(a.y); x[2] = __uint_as_float(a.z); x[3] = __uint_as_float(a.w);
+    x[4] = __uint_as_float(b.x); x[5] = __uint_as_float(b.y); x[6] = __uint_as_float(b.z); x[7] = __uint_as_float(b.w);
   } else {
+    const unsigned w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (j < left) {
-        store1(T.W, WDT, f + j, w[j]);
-        M[f + j] = (unsigned char)(mc[j >> 2] >> (8 * (j & 3)));
-        V[f + j] = (unsigned char)(vc[j >> 2] >> (8 * (j & 3)));
-      }
+    for (int j = 0; j < 4; ++j) {
+      x[2 * j] = __uint_as_float(w[j] << 16);
+      x[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
     }
-  }
-  // every lane has read the scales before the reductions above
-  if (lane == 0) {
-    T.ms[sb] = (unsigned char)mcode;
-    T.vs[sb] = (unsigned char)vcode;
   }
 }
 
+// Whole blocks b0 + warp, + 8, ... below b1 (at most 32 of a warp), eight elements a lane, all of it aligned. A lane copies what it will use to its
+// warp's ring in shared memory, some blocks ahead; no other lane touches that.
+constexpr int kRing8 = 48 * 1024;
 template <int WDT, int GDT>
-__global__ void __launch_bounds__(256) adamw_step8_kernel(const __grid_constant__ AwTable tab, AwLaunch l, const float* __restrict__ coef, int stride, AwStep s) {
+__device__ __forceinline__ void step8_blocks(const Arrays8& a, const Step8& s, unsigned long long key, long long b0, long long b1, int lane, int warp, char* ring) {
+  constexpr int kW = WDT == LORDO_F32 ? 1024 : 512, kG = GDT == LORDO_F32 ? 1024 : 512, kStage = kW + kG + 512, kStages = kRing8 / 8 / kStage;
+  const long long first = b0 + warp;
+  if (first >= b1) return;
+  const int count = (int)((b1 - first + 7) / 8);
+  const int mcodes = lane < count ? a.ms[first + 8 * lane] : 1, vcodes = lane < count ? a.vs[first + 8 * lane] : 1;
+  char* mine = ring + warp * (kStages * kStage);
+  const unsigned at = (unsigned)__cvta_generic_to_shared(mine);
+  const long long e0 = first * kAwBlock + 8 * lane;
+  auto fetch = [&](int x, int slot) {
+    if (x < count) {
+      const long long e = e0 + (long long)x * (8 * kAwBlock);
+      const unsigned to = at + slot * kStage;
+      copy8<WDT>(to + 16 * lane, a.W, e);
+      copy8<GDT>(to + kW + 16 * lane, a.G, e);
+      copy_async<8>(to + kW + kG + 8 * lane, a.m + e);
+      copy_async<8>(to + kW + kG + 256 + 8 * lane, a.v + e);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int x = 0; x < kStages - 1; ++x) fetch(x, x);
+  unsigned long long counter = counter4(key, e0);
+  int slot = 0, into = kStages - 1;
+  for (int x = 0; x < count; ++x) {
+    fetch(x + kStages - 1, into);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+    const char* p = mine + slot * kStage;
+    float g[8], w[8];
+    shared8<WDT>(p + 16 * lane, w);
+    shared8<GDT>(p + kW + 16 * lane, g);
+    const uint2 y = *reinterpret_cast<const uint2*>(p + kW + kG + 8 * lane), z = *reinterpret_cast<const uint2*>(p + kW + kG + 256 + 8 * lane);
+    unsigned mc[2] = {y.x, y.y}, vc[2] = {z.x, z.y};
+    int mcode = __shfl_sync(0xffffffffu, mcodes, x), vcode = __shfl_sync(0xffffffffu, vcodes, x);
+    step8_lane(s, counter, g, w, mc, vc, mcode, vcode);
+    const long long e = e0 + (long long)x * (8 * kAwBlock);
+    store8<WDT>(a.W, e, w);
+    *reinterpret_cast<uint2*>(a.m + e) = make_uint2(mc[0], mc[1]);
+    *reinterpret_cast<uint2*>(a.v + e) = make_uint2(vc[0], vc[1]);
+    if (lane == 0) {
+      a.ms[first + 8 * x] = (unsigned char)mcode;
+      a.vs[first + 8 * x] = (unsigned char)vcode;
+    }
+    counter += kGolden * (8 * kAwBlock / 4);
+    slot = slot + 1 == kStages ? 0 : slot + 1;
+    into = into + 1 == kStages ? 0 : into + 1;
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+
+template <int WDT, int GDT>
+__global__ void __launch_bounds__(256) adamw_step8_kernel(const __grid_constant__ AwTable tab, AwLaunch l, const float* __restrict__ coef, int stride, AwStep a) {
+  __shared__ __align__(16) char ring[kRing8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int k = (int)(blockIdx.x / l.units);
   const unsigned q = blockIdx.x - (unsigned)k * l.units;
   const int i = find_tensor(tab.start, l.count, q);
   const AwTensor T = l.tensors[i];
   const void* G = tab.G[i];
-  const unsigned long long key = mix64(s.key + kGolden * ((unsigned long long)T.index * l.K + k + 1));
+  const unsigned long long key = mix64(a.key + kGolden * ((unsigned long long)T.index * l.K + k + 1));
+  Step8 s;
+  s.b1 = a.b1; s.a1 = a.a1; s.b2 = a.b2; s.a2 = a.a2; s.root_inv_bc2 = a.root_inv_bc2; s.eps = a.eps;
+  s.keep = 1.f - a.lr * T.wd; s.lm = a.lr * a.omega * a.inv_bc1; s.lg = a.lr * a.a_omega;
   dep_begin();
-  const float c = coef ? __ldcg(coef + (long long)T.index * stride + k) : 1.f;
+  s.c = coef ? __ldcg(coef + (long long)T.index * stride + k) : 1.f;
   const long long base = (long long)k * T.n;
-  const long long b0 = (long long)(q - tab.start[i]) * (kAwPiece / kAwBlock);
-  const long long b1 = b0 + kAwPiece / kAwBlock < T.nb ? b0 + kAwPiece / kAwBlock : T.nb;
-  for (long long b = b0 + warp; b < b1; b += 8) step8_block<WDT, GDT>(T, G, s, c, key, k, base, b, lane);
+  Arrays8 x;
+  x.G = G ? reinterpret_cast<const char*>(G) + base * (GDT == LORDO_F32 ? 4 : 2) : nullptr;
+  x.W = reinterpret_cast<char*>(T.W) + base * (WDT == LORDO_F32 ? 4 : 2);
+  x.m = reinterpret_cast<unsigned char*>(T.m) + base;
+  x.v = reinterpret_cast<unsigned char*>(T.v) + base;
+  x.ms = T.ms + (long long)k * T.nb;
+  x.vs = T.vs + (long long)k * T.nb;
+  long long b0 = (long long)(q - tab.start[i]) * (l.piece / kAwBlock);
+  const long long b1 = b0 + l.piece / kAwBlock < T.nb ? b0 + l.piece / kAwBlock : T.nb;
+  if (G && (base & 7) == 0) {
+    const long long whole = T.n / kAwBlock < b1 ? T.n / kAwBlock : b1;
+    step8_blocks<WDT, GDT>(x, s, key, b0, whole, lane, warp, ring);
+    b0 = whole > b0 ? whole : b0;
+  }
+  // the last block of a worker, workers whose arrays begin at odd addresses, gradients by tokens
+  for (long long b = b0 + warp; b < b1; b += 8) {
+    const long long e = b * kAwBlock + 8 * lane;
+    const bool vec = (base & 7) == 0 && e + 8 <= T.n;
+    int mcode = x.ms[b], vcode = x.vs[b];
+    float g[8], w[8];
+    unsigned mc[2] = {0u, 0u}, vc[2] = {0u, 0u};
+    if (vec) {
+      if (G) load8<GDT>(x.G, e, g); else row_grad8(T, k, e, g);
+      load8<WDT>(x.W, e, w);
+      const uint2 y = *reinterpret_cast<const uint2*>(x.m + e), z = *reinterpret_cast<const uint2*>(x.v + e);
+      mc[0] = y.x; mc[1] = y.y; vc[0] = z.x; vc[1] = z.y;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        g[j] = w[j] = 0.f;
+        if (e + j < T.n) {
+          g[j] = G ? load1(x.G, GDT, e + j) : row_grad(T, k, e + j);
+          w[j] = load1(x.W, WDT, e + j);
+          mc[j >> 2] |= (unsigned)x.m[e + j] << (8 * (j & 3));
+          vc[j >> 2] |= (unsigned)x.v[e + j] << (8 * (j & 3));
+        }
+      }
+    }
+    step8_lane(s, counter4(key, e), g, w, mc, vc, mcode, vcode);
+    if (vec) {
+      store8<WDT>(x.W, e, w);
+      *reinterpret_cast<uint2*>(x.m + e) = make_uint2(mc[0], mc[1]);
+      *reinterpret_cast<uint2*>(x.v + e) = make_uint2(vc[0], vc[1]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (e + j < T.n) {
+          store1(x.W, WDT, e + j, w[j]);
+          x.m[e + j] = (unsigned char)(mc[j >> 2] >> (8 * (j & 3)));
+          x.v[e + j] = (unsigned char)(vc[j >> 2] >> (8 * (j & 3)));
+        }
+      }
+    }
+    if (lane == 0) {  // every lane has read the old scales before the reductions
+      x.ms[b] = (unsigned char)mcode;
+      x.vs[b] = (unsigned char)vcode;
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -514,14 +634,14 @@ __device__ __forceinline__ void outer_mean8(const AwTensor& T, int K, float inv_
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     a[j] *= inv_k;
-    if (SECOND) a[j] = sqrtf(a[j]);
+    if (SECOND) a[j] = root(a[j]);
   }
   const int code = scale_code(__reduce_max_sync(0xffffffffu, top8(a)));
   const float inv = pow2(254 - code);
   unsigned c[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const unsigned long long r = bits4(key, e + 4 * h);
+    const unsigned long long r = mix64(counter4(key, e) + h * kGolden);
     const unsigned u[4] = {first16(r, 0), first16(r, 1), first16(r, 2), first16(r, 3)};
     c[h] = pack8<SECOND, false>(a + 4 * h, inv, u);
   }

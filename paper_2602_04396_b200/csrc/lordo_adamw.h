@@ -5,7 +5,11 @@
 namespace lordo {
 
 constexpr int kAwBlock = 256;    // elements per scale of the 8-bit moments
-constexpr int kAwPiece = 8192;   // elements of one worker's tensor that a CTA of the step works on
+// Elements of one worker's tensor that a CTA of the step works on: 2048 (eight a thread) to 32768, about one for each of 148 * 8 CTAs where there are fewer.
+inline long long aw_piece(long long elements) {
+  const long long p = (elements / (148 * 8) + 2047) / 2048 * 2048;
+  return p < 2048 ? 2048 : p > 32768 ? 32768 : p;
+}
 constexpr int kAwChunk = 32768;  // elements of one worker's tensor behind a partial sum of squares
 constexpr int kAwOuter = 4096;   // elements of a tensor that a CTA of the synchronisation works on
 constexpr int kAwTable = 512;    // tensors of one launch
@@ -46,6 +50,7 @@ struct AwLaunch {
   int count, K;
   unsigned units;           // per worker
   int w_dt, g_dt, small;    // small: 8-bit moments
+  int piece;                // elements behind a unit of the step
 };
 
 struct AwClip {

@@ -43,6 +43,7 @@ struct lordo_adamw_ctx {
   float* d_coef = nullptr;
   size_t n_tickets = 0;
   unsigned total_chunks = 0;
+  int piece = 0;
   int64_t steps = 0, outers = 0, launches = 0;
   std::string err;
 };
@@ -80,7 +81,7 @@ int validate(const lordo_adamw_config* cfg) {
     elements += t.n;
   }
   // blocks of a launch and partial sums are counted in 32 bits
-  if ((elements / kAwOuter + cfg->n_tensors) * cfg->K > (1ll << 30)) return LORDO_ERR_UNSUPPORTED;
+  if ((elements / 2048 + cfg->n_tensors) * cfg->K > (1ll << 30)) return LORDO_ERR_UNSUPPORTED;
   return LORDO_OK;
 }
 
@@ -102,6 +103,9 @@ size_t build(lordo_adamw_ctx* c, const lordo_adamw_buffers* buf, char* base) {
   c->groups.clear(); c->tables.clear(); c->h_tensors.assign(nt, AwTensor());
   c->table_of.assign(nt, -1);
   c->total_chunks = 0;
+  long long elements = 0;
+  for (int i = 0; i < nt; ++i) elements += cfg.tensors[i].n * K;
+  c->piece = (int)aw_piece(elements);
   for (int first = 0; first < nt; first += kAwTable) {
     c->groups.emplace_back();
     Group& g = c->groups.back();
@@ -115,7 +119,7 @@ size_t build(lordo_adamw_ctx* c, const lordo_adamw_buffers* buf, char* base) {
       g.norm.start[x] = g.chunks; g.step.start[x] = g.pieces;
       g.outer.push_back(g.blocks);
       g.chunks += (unsigned)cdiv(n, kAwChunk);
-      g.pieces += (unsigned)cdiv(n, kAwPiece);
+      g.pieces += (unsigned)cdiv(n, c->piece);
       g.blocks += (unsigned)cdiv(n, kAwOuter);
     }
     g.norm.start[g.count] = g.chunks; g.step.start[g.count] = g.pieces;
@@ -155,7 +159,7 @@ size_t build(lordo_adamw_ctx* c, const lordo_adamw_buffers* buf, char* base) {
 }
 
 AwLaunch launch_of(const lordo_adamw_ctx* c, const Group& g, unsigned units) {
-  return AwLaunch{c->d_tensors + g.first, g.count, c->cfg.K, units, c->cfg.w_dtype, c->cfg.g_dtype, c->cfg.states == LORDO_STATES_8BIT};
+  return AwLaunch{c->d_tensors + g.first, g.count, c->cfg.K, units, c->cfg.w_dtype, c->cfg.g_dtype, c->cfg.states == LORDO_STATES_8BIT, c->piece};
 }
 
 int check_launch(lordo_adamw_ctx* c, const char* what) {
