@@ -230,78 +230,97 @@ __device__ __forceinline__ int scale_code(unsigned top) {
 }
 __device__ __forceinline__ float pow2(int code) { return __int_as_float(code << 23); }  // 2^(code - 127), code in [1, 254]
 
-// E4M3 code of a magnitude t < 256, rounded down after (u + 1/2) / 65536 of a step was added; u16 = 16 u. Below 2^-6 the steps are 2^-9
-// wide, as they are for t + 2^-6. Infinities and NaN become NaN.
-__device__ __forceinline__ unsigned code8(float t, unsigned u16) {
-  const bool sub = t < 0.015625f;
-  const unsigned b = __float_as_uint(fabsf(sub ? t + 0.015625f : t));
-  const int code = (int)((b + u16 + 8u) >> 20) - (sub ? 968 : 960);
-  return (unsigned)(code > 127 ? 127 : code);
+// E4M3 code of a magnitude t < 256, rounded down after (u + 1/2) / 65536 of a step was added; u256 = 256 u + 128. A float's own bits are that code
+// once t is scaled by 2^-120: the exponent's bias becomes E4M3's, floats below 2^-126 are its subnormal codes, and three bits of the mantissa stand
+// above 20 that are dropped. Infinities and NaN become NaN.
+__device__ __forceinline__ unsigned code8(float t, unsigned u256) {
+  const unsigned c = (__float_as_uint(fabsf(t) * 0x1p-120f) + (u256 >> 4)) >> 20;
+  return c > 127u ? 127u : c;
 }
-// The same for finite t in [2^-6, 256), in the top seven bits behind the sign's place.
-__device__ __forceinline__ unsigned code8_normal(float t, unsigned u16) { return (__float_as_uint(t) + u16 + (8u - (960u << 20))) << 4; }
 
 // Four values of E4M3 codes.
-__device__ __forceinline__ void values8(unsigned c, float* x) {
+__device__ __forceinline__ void values8(unsigned c, float2 (&x)[2]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(c >> (16 * h)), __NV_E4M3);
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r));
-    x[2 * h] = f.x;
-    x[2 * h + 1] = f.y;
+    x[h] = __half22float2(*reinterpret_cast<const __half2*>(&r));
   }
 }
 
-// 16 times the 16 random bits of element j of four, for the first moment and for the second
+// 256 u + 128 of element j of four, u its 16 random bits: one byte permutation; the same for the second moment.
 __device__ __forceinline__ unsigned first16(unsigned long long r, int j) {
-  const unsigned w = j < 2 ? (unsigned)r : (unsigned)(r >> 32);
-  return (j & 1 ? w >> 12 : w << 4) & 0xFFFF0u;
+  return __byte_perm(j < 2 ? (unsigned)r : (unsigned)(r >> 32), 0x00000080u, j & 1 ? 0x7324 : 0x7104);
 }
-__device__ __forceinline__ unsigned second16(unsigned first) { return (first * 40503u) & 0xFFFF0u; }
+__device__ __forceinline__ unsigned second16(unsigned first) { return (((first - 128u) * 40503u) & 0xFFFF00u) | 128u; }
 
-constexpr unsigned kInfBits = 0x7F800000u;
-
-__device__ __forceinline__ unsigned top8(const float (&x)[8]) {
-  unsigned t = 0u;
-#pragma unroll
-  for (int j = 0; j < 8; j += 2) t = __vimax3_u32(t, __float_as_uint(x[j]) & 0x7FFFFFFFu, __float_as_uint(x[j + 1]) & 0x7FFFFFFFu);
-  return t;
-}
-__device__ __forceinline__ unsigned low8(const float (&x)[8]) {
-  unsigned t = 0xFFFFFFFFu;
-#pragma unroll
-  for (int j = 0; j < 8; j += 2) t = __vimin3_u32(t, __float_as_uint(x[j]) & 0x7FFFFFFFu, __float_as_uint(x[j + 1]) & 0x7FFFFFFFu);
-  return t;
-}
-
-// Codes of four elements. NORMAL: every |x| inv lies in [2^-6, 256).
-template <bool SECOND, bool NORMAL>
-__device__ __forceinline__ unsigned pack8(const float* x, float inv, const unsigned (&u16)[4]) {
-  unsigned b[4];
+// Bits of the largest magnitude of a lane's eight values, of either sign and of none below 0; of the least of the latter.
+__device__ __forceinline__ unsigned top_signed(const float2 (&x)[4]) {
+  int up = 0;
+  unsigned down = 0u;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const unsigned u = SECOND ? second16(u16[j]) : u16[j];
-    const unsigned bits = __float_as_uint(x[j]);
-    if (NORMAL) {
-      b[j] = code8_normal(fabsf(x[j]) * inv, u);
-    } else {
-      unsigned c = code8(fabsf(x[j]) * inv, u);
-      if (SECOND && c == 0u && x[j] > 0.f) c = 1u;
-      b[j] = c << 24;
+    up = __vimax3_s32(up, __float_as_int(x[j].x), __float_as_int(x[j].y));
+    down = __vimax3_u32(down, __float_as_uint(x[j].x), __float_as_uint(x[j].y));
+  }
+  const unsigned low = down & 0x7FFFFFFFu;  // of the negative ones where there are any
+  return (unsigned)up > low ? (unsigned)up : low;
+}
+__device__ __forceinline__ unsigned top_positive(const float2 (&x)[4]) {
+  unsigned t = 0u;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) t = __vimax3_u32(t, __float_as_uint(x[j].x), __float_as_uint(x[j].y));
+  return t;
+}
+__device__ __forceinline__ unsigned low_positive(const float2 (&x)[4]) {
+  unsigned t = 0xFFFFFFFFu;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) t = __vimin3_u32(t, __float_as_uint(x[j].x), __float_as_uint(x[j].y));
+  return t;
+}
+
+// 16 x + y. Written out: as a shift by four, nvcc 12.9 lost it where x came from one half of a packed product and the result's top byte was taken.
+__device__ __forceinline__ unsigned mad16(unsigned x, unsigned y) {
+  unsigned r;
+  asm("mad.lo.u32 %0, %1, 16, %2;" : "=r"(r) : "r"(x), "r"(y));
+  return r;
+}
+
+enum Pack8 { PACK_SIGNED, PACK_POSITIVE, PACK_ANY };
+// Codes of four values. inv is 2^-120 times the reciprocal of the scale for all but ANY, where it is that itself: there a value may be anything, and
+// positive ones do not become zero with SECOND (the smallest code instead). u256: first16 of the four.
+template <int KIND, bool SECOND>
+__device__ __forceinline__ unsigned pack8(const float2 (&x)[2], float inv, const unsigned (&u256)[4]) {
+  unsigned b[4];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const float2 t = KIND == PACK_ANY ? x[h] : __fmul2_rn(x[h], make_float2(inv, inv));
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float y = j ? t.y : t.x;
+      const unsigned u = SECOND ? second16(u256[2 * h + j]) : u256[2 * h + j];
+      if (KIND == PACK_ANY) {
+        unsigned c = code8(y * inv, u);
+        if (SECOND && c == 0u && y > 0.f) c = 1u;
+        b[2 * h + j] = (c << 24) | (SECOND ? 0u : __float_as_uint(y) & 0x80000000u);
+      } else {
+        const unsigned c = mad16(__float_as_uint(y), u);  // the code in bits 24 to 30
+        b[2 * h + j] = KIND == PACK_SIGNED ? (c & 0x7FFFFFFFu) | (__float_as_uint(y) & 0x80000000u) : c;
+      }
     }
-    b[j] = SECOND ? b[j] : (b[j] & 0x7FFFFFFFu) | (bits & 0x80000000u);
   }
   return __byte_perm(__byte_perm(b[0], b[1], 0x0073), __byte_perm(b[2], b[3], 0x0073), 0x5410);  // the top byte of each
 }
 
 // sqrt(v) by one of Newton's (Heron's) steps on r^2 = v from r = v rsqrt(v), whose derivative 2 r is 2 / rsqrt(v): of normal numbers off by less than
 // a unit in the last place, as a rule rounded to the nearest. The step is not a number for 0 (and below 2^-126), infinity and NaN; the maximum
-// then takes v 1e-20, which is 0, infinity and NaN, and below the root of any other v. Seven instructions without a branch; sqrtf has one.
-__device__ __forceinline__ float root(float v) {
-  float y;
-  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(v));
-  const float r = v * y;
-  return fmaxf(fmaf(fmaf(-r, r, v), 0.5f * y, r), v * 1e-20f);
+// then takes v 1e-20, which is 0, infinity and NaN, and below the root of any other v. No branch; sqrtf has one.
+__device__ __forceinline__ float2 root(float2 v) {
+  float2 y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(v.x));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(v.y));
+  const float2 r = __fmul2_rn(v, y), minus = __fmul2_rn(v, make_float2(-y.x, -y.y));
+  const float2 x = __ffma2_rn(__ffma2_rn(minus, r, v), __fmul2_rn(y, make_float2(0.5f, 0.5f)), r), least = __fmul2_rn(v, make_float2(1e-20f, 1e-20f));
+  return make_float2(fmaxf(x.x, least.x), fmaxf(x.y, least.y));
 }
 __device__ __forceinline__ float reciprocal(float x) {
   float y;
@@ -313,44 +332,52 @@ struct Step8 {  // constants of a step, of its worker and tensor
   float c, b1, a1, b2, a2, keep, lm, lg, root_inv_bc2, eps;
 };
 
-// A lane's eight elements of a block of 256 of one worker's tensor: codes in, codes and scales out. The scales are powers of two, so that b1 (m8 S) is
-// (b1 S) m8 to the last bit, and b2 (s8 S)^2 is (b2 S^2) s8^2.
-__device__ __forceinline__ void step8_lane(const Step8& s, unsigned long long counter, float (&g)[8], float (&w)[8], unsigned (&mc)[2], unsigned (&vc)[2],
-                                           int& mcode, int& vcode) {
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// A lane's eight elements of a block of 256 of one worker's tensor: codes in, codes and scales out. Arithmetic goes by pairs of elements in one
+// instruction each (the issue slots are what a step is short of), every product and sum rounded on its own. The scales are powers of two, so that
+// b1 (m8 S) is (b1 S) m8 to the last bit, and b2 (s8 S)^2 is (b2 S^2) s8^2. The weights' quotient is good to two units in the last place.
+__device__ __forceinline__ void step8_lane(const Step8& s, unsigned long long counter, const float2 (&g)[4], float2 (&w)[4], unsigned (&mc)[2],
+                                           unsigned (&vc)[2], int& mcode, int& vcode) {
   const float ms = pow2(mcode), vs = pow2(vcode);
-  const float b1 = s.b1 * ms, b2 = s.b2 * (vs * vs);
-  float m[8], r[8];
+  const float2 b1 = both(s.b1 * ms), b2 = both(s.b2 * (vs * vs)), c = both(s.c), a1 = both(s.a1), a2 = both(s.a2);
+  const float2 lm = both(-s.lm), lg = both(-s.lg), keep = both(s.keep), q = both(s.root_inv_bc2), eps = both(s.eps);
+  float2 m[4], r[4];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    values8(mc[h], m + 4 * h);
-    values8(vc[h], r + 4 * h);
-  }
+    float2 x[2], y[2];
+    values8(mc[h], x);
+    values8(vc[h], y);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float x = __fmul_rn(g[j], s.c);
-    m[j] = __fadd_rn(__fmul_rn(b1, m[j]), __fmul_rn(s.a1, x));
-    r[j] = root(__fadd_rn(__fmul_rn(b2, r[j] * r[j]), __fmul_rn(__fmul_rn(s.a2, x), x)));
-    w[j] = fmaf(-(s.lm * m[j] + s.lg * x), reciprocal(fmaf(r[j], s.root_inv_bc2, s.eps)), w[j] * s.keep);
+    for (int j = 0; j < 2; ++j) {
+      const int at = 2 * h + j;
+      const float2 z = __fmul2_rn(g[at], c);
+      m[at] = __fadd2_rn(__fmul2_rn(b1, x[j]), __fmul2_rn(a1, z));
+      r[at] = root(__fadd2_rn(__fmul2_rn(b2, __fmul2_rn(y[j], y[j])), __fmul2_rn(__fmul2_rn(a2, z), z)));
+      const float2 d = __ffma2_rn(r[at], q, eps);
+      w[at] = __ffma2_rn(__ffma2_rn(lm, m[at], __fmul2_rn(lg, z)), make_float2(reciprocal(d.x), reciprocal(d.y)), __fmul2_rn(w[at], keep));
+    }
   }
-  const unsigned mtop = __reduce_max_sync(0xffffffffu, top8(m)), vtop = __reduce_max_sync(0xffffffffu, top8(r));
+  const unsigned mtop = __reduce_max_sync(0xffffffffu, top_signed(m)), vtop = __reduce_max_sync(0xffffffffu, top_positive(r));
   mcode = scale_code(mtop);
   vcode = scale_code(vtop);
+  // scales above 2^6 (their reciprocal's 2^-120 would not be a normal number), infinities, NaN; and sqrt(v) of 0 or below half the smallest code
+  constexpr unsigned kLarge = (127u + 14u) << 23;
   const float mi = pow2(254 - mcode), vi = pow2(254 - vcode);
-  // magnitudes below 2^-6 of the grid, which take half as many instructions again, are rare: a block has them or it has not
-  const bool low = __uint_as_float(low8(m)) * mi < 0.015625f || __uint_as_float(low8(r)) * vi < 0.015625f;
-  const bool slow = __any_sync(0xffffffffu, low) || mtop >= kInfBits || vtop >= kInfBits;
+  const bool slow = mtop >= kLarge || vtop >= kLarge || __any_sync(0xffffffffu, __uint_as_float(low_positive(r)) * vi < 0x1p-9f);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const unsigned long long x = mix64(counter + h * kGolden);
     unsigned u[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) u[j] = first16(x, j);
+    const float2 mh[2] = {m[2 * h], m[2 * h + 1]}, rh[2] = {r[2 * h], r[2 * h + 1]};
     if (slow) {
-      mc[h] = pack8<false, false>(m + 4 * h, mi, u);
-      vc[h] = pack8<true, false>(r + 4 * h, vi, u);
+      mc[h] = pack8<PACK_ANY, false>(mh, mi, u);
+      vc[h] = pack8<PACK_ANY, true>(rh, vi, u);
     } else {
-      mc[h] = pack8<false, true>(m + 4 * h, mi, u);
-      vc[h] = pack8<true, true>(r + 4 * h, vi, u);
+      mc[h] = pack8<PACK_SIGNED, false>(mh, mi * 0x1p-120f, u);
+      vc[h] = pack8<PACK_POSITIVE, true>(rh, vi * 0x1p-120f, u);
     }
   }
 }
@@ -373,19 +400,27 @@ __device__ __forceinline__ void copy8(unsigned to, const void* base, long long a
   if constexpr (DT == LORDO_F32) copy_async<16>(to + 512, p + 16);
 }
 template <int DT>
-__device__ __forceinline__ void shared8(const char* from, float (&x)[8]) {
-  const uint4 a = *reinterpret_cast<const uint4*>(from);
+__device__ __forceinline__ void widen8(const uint4& a, const uint4& b, float2 (&x)[4]) {  // b: fp32 only
   if constexpr (DT == LORDO_F32) {
-    const uint4 b = *reinterpret_cast<const uint4*>(from + 512);
-    x[0] = __uint_as_float(a.x); x[1] = __uint_as_float(a.y); x[2] = __uint_as_float(a.z); x[3] = __uint_as_float(a.w);
-    x[4] = __uint_as_float(b.x); x[5] = __uint_as_float(b.y); x[6] = __uint_as_float(b.z); x[7] = __uint_as_float(b.w);
+    x[0] = make_float2(__uint_as_float(a.x), __uint_as_float(a.y)); x[1] = make_float2(__uint_as_float(a.z), __uint_as_float(a.w));
+    x[2] = make_float2(__uint_as_float(b.x), __uint_as_float(b.y)); x[3] = make_float2(__uint_as_float(b.z), __uint_as_float(b.w));
   } else {
     const unsigned w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[2 * j] = __uint_as_float(w[j] << 16);
-      x[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-    }
+    for (int j = 0; j < 4; ++j) x[j] = make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xFFFF0000u));
+  }
+}
+template <int DT>
+__device__ __forceinline__ void shared8(const char* from, float2 (&x)[4]) {
+  widen8<DT>(*reinterpret_cast<const uint4*>(from), DT == LORDO_F32 ? *reinterpret_cast<const uint4*>(from + 512) : uint4{}, x);
+}
+template <int DT>
+__device__ __forceinline__ void put8(char* to, const float2 (&x)[4]) {
+  if constexpr (DT == LORDO_F32) {
+    reinterpret_cast<float4*>(to)[0] = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
+    reinterpret_cast<float4*>(to)[1] = make_float4(x[2].x, x[2].y, x[3].x, x[3].y);
+  } else {
+    *reinterpret_cast<uint4*>(to) = make_uint4(pack_bf16x2(x[0].x, x[0].y), pack_bf16x2(x[1].x, x[1].y), pack_bf16x2(x[2].x, x[2].y), pack_bf16x2(x[3].x, x[3].y));
   }
 }
 
@@ -394,57 +429,70 @@ __device__ __forceinline__ void shared8(const char* from, float (&x)[8]) {
 constexpr int kRing8 = 48 * 1024;
 template <int WDT, int GDT>
 __device__ __forceinline__ void step8_blocks(const Arrays8& a, const Step8& s, unsigned long long key, long long b0, long long b1, int lane, int warp, char* ring) {
-  constexpr int kW = WDT == LORDO_F32 ? 1024 : 512, kG = GDT == LORDO_F32 ? 1024 : 512, kStage = kW + kG + 512, kStages = kRing8 / 8 / kStage;
+  constexpr int kWb = WDT == LORDO_F32 ? 4 : 2, kGb = GDT == LORDO_F32 ? 4 : 2, kStep = 8 * kAwBlock;  // elements from block to block
+  constexpr int kM = 256 * (kWb + kGb), kStage = kM + 512, kStages = kRing8 / 8 / kStage;
   const long long first = b0 + warp;
   if (first >= b1) return;
   const int count = (int)((b1 - first + 7) / 8);
-  const int mcodes = lane < count ? a.ms[first + 8 * lane] : 1, vcodes = lane < count ? a.vs[first + 8 * lane] : 1;
-  char* mine = ring + warp * (kStages * kStage);
-  const unsigned at = (unsigned)__cvta_generic_to_shared(mine);
+  int mcodes = lane < count ? a.ms[first + 8 * lane] : 1, vcodes = lane < count ? a.vs[first + 8 * lane] : 1;
   const long long e0 = first * kAwBlock + 8 * lane;
-  auto fetch = [&](int x, int slot) {
-    if (x < count) {
-      const long long e = e0 + (long long)x * (8 * kAwBlock);
-      const unsigned to = at + slot * kStage;
-      copy8<WDT>(to + 16 * lane, a.W, e);
-      copy8<GDT>(to + kW + 16 * lane, a.G, e);
-      copy_async<8>(to + kW + kG + 8 * lane, a.m + e);
-      copy_async<8>(to + kW + kG + 256 + 8 * lane, a.v + e);
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
+  char* mine = ring + warp * (kStages * kStage) + 16 * lane;  // of W and G; codes 8 * lane in
+  const unsigned at = (unsigned)__cvta_generic_to_shared(mine);
+  char* pw = reinterpret_cast<char*>(a.W) + e0 * kWb;
+  const char* pg = reinterpret_cast<const char*>(a.G) + e0 * kGb;
+  unsigned char *pm = a.m + e0, *pv = a.v + e0;
+  auto fetch = [&](unsigned slot) {
+    copy8<WDT>(at + slot, pw, 0);
+    copy8<GDT>(at + slot + 256 * kWb, pg, 0);
+    copy_async<8>(at + slot + kM - 8 * lane, pm);
+    copy_async<8>(at + slot + kM + 256 - 8 * lane, pv);
+  };
+  auto advance = [&]() {
+    pw += kStep * kWb;
+    pg += kStep * kGb;
+    pm += kStep;
+    pv += kStep;
   };
 #pragma unroll
-  for (int x = 0; x < kStages - 1; ++x) fetch(x, x);
+  for (int x = 0; x < kStages - 1; ++x) {
+    if (x < count) fetch(x * kStage);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    advance();
+  }
   unsigned long long counter = counter4(key, e0);
-  int slot = 0, into = kStages - 1;
+  unsigned slot = 0, into = (kStages - 1) * kStage;
   for (int x = 0; x < count; ++x) {
-    fetch(x + kStages - 1, into);
-    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
-    const char* p = mine + slot * kStage;
-    float g[8], w[8];
-    shared8<WDT>(p + 16 * lane, w);
-    shared8<GDT>(p + kW + 16 * lane, g);
-    const uint2 y = *reinterpret_cast<const uint2*>(p + kW + kG + 8 * lane), z = *reinterpret_cast<const uint2*>(p + kW + kG + 256 + 8 * lane);
+    if (x + kStages - 1 < count) fetch(into);
+    asm volatile("cp.async.commit_group;\ncp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+    const char* p = mine + slot;
+    float2 g[4], w[4];
+    shared8<WDT>(p, w);
+    shared8<GDT>(p + 256 * kWb, g);
+    const uint2 y = *reinterpret_cast<const uint2*>(p + kM - 8 * lane), z = *reinterpret_cast<const uint2*>(p + kM + 256 - 8 * lane);
     unsigned mc[2] = {y.x, y.y}, vc[2] = {z.x, z.y};
     int mcode = __shfl_sync(0xffffffffu, mcodes, x), vcode = __shfl_sync(0xffffffffu, vcodes, x);
     step8_lane(s, counter, g, w, mc, vc, mcode, vcode);
-    const long long e = e0 + (long long)x * (8 * kAwBlock);
-    store8<WDT>(a.W, e, w);
-    *reinterpret_cast<uint2*>(a.m + e) = make_uint2(mc[0], mc[1]);
-    *reinterpret_cast<uint2*>(a.v + e) = make_uint2(vc[0], vc[1]);
-    if (lane == 0) {
-      a.ms[first + 8 * x] = (unsigned char)mcode;
-      a.vs[first + 8 * x] = (unsigned char)vcode;
+    constexpr int kBack = (kStages - 1) * kStep;
+    put8<WDT>(pw - kBack * kWb, w);
+    *reinterpret_cast<uint2*>(pm - kBack) = make_uint2(mc[0], mc[1]);
+    *reinterpret_cast<uint2*>(pv - kBack) = make_uint2(vc[0], vc[1]);
+    if (lane == x) {
+      mcodes = mcode;
+      vcodes = vcode;
     }
-    counter += kGolden * (8 * kAwBlock / 4);
-    slot = slot + 1 == kStages ? 0 : slot + 1;
-    into = into + 1 == kStages ? 0 : into + 1;
+    advance();
+    counter += kGolden * (kStep / 4);
+    into = slot;
+    slot = slot + kStage == kStages * kStage ? 0u : slot + kStage;
   }
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  if (lane < count) {
+    a.ms[first + 8 * lane] = (unsigned char)mcodes;
+    a.vs[first + 8 * lane] = (unsigned char)vcodes;
+  }
 }
 
 template <int WDT, int GDT>
-__global__ void __launch_bounds__(256) adamw_step8_kernel(const __grid_constant__ AwTable tab, AwLaunch l, const float* __restrict__ coef, int stride, AwStep a) {
+__global__ void __launch_bounds__(256, 4) adamw_step8_kernel(const __grid_constant__ AwTable tab, AwLaunch l, const float* __restrict__ coef, int stride, AwStep a) {
   __shared__ __align__(16) char ring[kRing8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int k = (int)(blockIdx.x / l.units);
@@ -478,35 +526,41 @@ __global__ void __launch_bounds__(256) adamw_step8_kernel(const __grid_constant_
     const long long e = b * kAwBlock + 8 * lane;
     const bool vec = (base & 7) == 0 && e + 8 <= T.n;
     int mcode = x.ms[b], vcode = x.vs[b];
-    float g[8], w[8];
+    float ge[8], we[8];
     unsigned mc[2] = {0u, 0u}, vc[2] = {0u, 0u};
     if (vec) {
-      if (G) load8<GDT>(x.G, e, g); else row_grad8(T, k, e, g);
-      load8<WDT>(x.W, e, w);
+      if (G) load8<GDT>(x.G, e, ge); else row_grad8(T, k, e, ge);
+      load8<WDT>(x.W, e, we);
       const uint2 y = *reinterpret_cast<const uint2*>(x.m + e), z = *reinterpret_cast<const uint2*>(x.v + e);
       mc[0] = y.x; mc[1] = y.y; vc[0] = z.x; vc[1] = z.y;
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        g[j] = w[j] = 0.f;
+        ge[j] = we[j] = 0.f;
         if (e + j < T.n) {
-          g[j] = G ? load1(x.G, GDT, e + j) : row_grad(T, k, e + j);
-          w[j] = load1(x.W, WDT, e + j);
+          ge[j] = G ? load1(x.G, GDT, e + j) : row_grad(T, k, e + j);
+          we[j] = load1(x.W, WDT, e + j);
           mc[j >> 2] |= (unsigned)x.m[e + j] << (8 * (j & 3));
           vc[j >> 2] |= (unsigned)x.v[e + j] << (8 * (j & 3));
         }
       }
     }
+    float2 g[4], w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      g[j] = make_float2(ge[2 * j], ge[2 * j + 1]);
+      w[j] = make_float2(we[2 * j], we[2 * j + 1]);
+    }
     step8_lane(s, counter4(key, e), g, w, mc, vc, mcode, vcode);
     if (vec) {
-      store8<WDT>(x.W, e, w);
+      put8<WDT>(reinterpret_cast<char*>(x.W) + e * (WDT == LORDO_F32 ? 4 : 2), w);
       *reinterpret_cast<uint2*>(x.m + e) = make_uint2(mc[0], mc[1]);
       *reinterpret_cast<uint2*>(x.v + e) = make_uint2(vc[0], vc[1]);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (e + j < T.n) {
-          store1(x.W, WDT, e + j, w[j]);
+          store1(x.W, WDT, e + j, j & 1 ? w[j >> 1].y : w[j >> 1].x);
           x.m[e + j] = (unsigned char)(mc[j >> 2] >> (8 * (j & 3)));
           x.v[e + j] = (unsigned char)(vc[j >> 2] >> (8 * (j & 3)));
         }
@@ -609,7 +663,7 @@ __device__ __forceinline__ void outer_mean8(const AwTensor& T, int K, float inv_
   unsigned char* C = reinterpret_cast<unsigned char*>(SECOND ? T.v : T.m);
   unsigned char* S = SECOND ? T.vs : T.ms;
   const bool vec = left == 8 && (T.n & 7) == 0;
-  float a[8] = {};
+  float2 a[4] = {};
   for (int k = 0; k < K; ++k) {
     const float scale = pow2(S[(long long)k * T.nb + b]);
     const unsigned char* p = C + (long long)k * T.n + e;
@@ -622,28 +676,31 @@ __device__ __forceinline__ void outer_mean8(const AwTensor& T, int K, float inv_
       for (int j = 0; j < 8; ++j)
         if (j < left) c[j >> 2] |= (unsigned)p[j] << (8 * (j & 3));
     }
-    float x[8];
-    values8(c[0], x);
-    values8(c[1], x + 4);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      x[j] *= scale;
-      a[j] += SECOND ? x[j] * x[j] : x[j];
+    for (int h = 0; h < 2; ++h) {
+      float2 x[2];
+      values8(c[h], x);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float2 y = __fmul2_rn(x[j], both(scale));
+        a[2 * h + j] = SECOND ? __ffma2_rn(y, y, a[2 * h + j]) : __fadd2_rn(a[2 * h + j], y);
+      }
     }
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    a[j] *= inv_k;
+  for (int j = 0; j < 4; ++j) {
+    a[j] = __fmul2_rn(a[j], both(inv_k));
     if (SECOND) a[j] = root(a[j]);
   }
-  const int code = scale_code(__reduce_max_sync(0xffffffffu, top8(a)));
+  const int code = scale_code(__reduce_max_sync(0xffffffffu, SECOND ? top_positive(a) : top_signed(a)));
   const float inv = pow2(254 - code);
   unsigned c[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const unsigned long long r = mix64(counter4(key, e) + h * kGolden);
     const unsigned u[4] = {first16(r, 0), first16(r, 1), first16(r, 2), first16(r, 3)};
-    c[h] = pack8<SECOND, false>(a + 4 * h, inv, u);
+    const float2 x[2] = {a[2 * h], a[2 * h + 1]};
+    c[h] = pack8<PACK_ANY, SECOND>(x, inv, u);
   }
   for (int k = 0; k < K; ++k) {
     unsigned char* p = C + (long long)k * T.n + e;
