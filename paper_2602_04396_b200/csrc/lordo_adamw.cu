@@ -101,29 +101,39 @@ __global__ void __launch_bounds__(256) adamw_norm_kernel(const __grid_constant__
   dep_begin();
   double s = 0.0;
   if (G) {
-    const long long e0 = (long long)(q - tab.start[i]) * kAwChunk;
-    const long long e1 = e0 + kAwChunk < n ? e0 + kAwChunk : n;
+    const long long e0 = (long long)(q - tab.start[i]) * c.chunk;
+    const long long e1 = e0 + c.chunk < n ? e0 + c.chunk : n;
     const long long f0 = (long long)k * n + e0, f1 = (long long)k * n + e1;
     const long long a0 = (f0 + 7) & ~7ll, a1 = f1 & ~7ll;
-    for (long long f = a0 + 8 * t; f < a1; f += 2 * 2048) {
-      float x[2][8];
+    double part[2] = {0.0, 0.0};
+    for (long long f = a0 + 8 * t; f < a1; f += 4 * 2048) {
+      uint4 x[4][GDT == LORDO_F32 ? 2 : 1];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        if (f + u * 2048 < a1) {
-          load8<GDT>(G, f + u * 2048, x[u]);
-        } else {
+      for (int u = 0; u < 4; ++u) {
+        const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(G) + (f + u * 2048) * (GDT == LORDO_F32 ? 4 : 2));
 #pragma unroll
-          for (int j = 0; j < 8; ++j) x[u][j] = 0.f;
-        }
+        for (int h = 0; h < (GDT == LORDO_F32 ? 2 : 1); ++h) x[u][h] = f + u * 2048 < a1 ? p[h] : make_uint4(0u, 0u, 0u, 0u);
       }
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {  // eight squares in fp32, the rest in fp64
+      for (int u = 0; u < 4; ++u) {  // eight squares in fp32, the rest in fp64
         float sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum += x[u][j] * x[u][j];
-        s += (double)sum;
+        for (int h = 0; h < (GDT == LORDO_F32 ? 2 : 1); ++h) {
+          const unsigned w[4] = {x[u][h].x, x[u][h].y, x[u][h].z, x[u][h].w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (GDT == LORDO_F32) {
+              sum += __uint_as_float(w[j]) * __uint_as_float(w[j]);
+            } else {
+              const float lo = __uint_as_float(w[j] << 16), hi = __uint_as_float(w[j] & 0xFFFF0000u);
+              sum += lo * lo + hi * hi;
+            }
+          }
+        }
+        part[u & 1] += (double)sum;
       }
     }
+    s = part[0] + part[1];
     const long long edge = t < 8 ? f0 + t : (a1 > a0 ? a1 : a0) + t - 8;  // elements before the first and behind the last vector
     if (t < 16 && edge < f1 && (t >= 8 || edge < a0)) {
       const float x = load1(G, GDT, edge);
@@ -494,7 +504,7 @@ __device__ __forceinline__ void step8_blocks(const Arrays8& a, const Step8& s, u
 template <int WDT, int GDT>
 __global__ void __launch_bounds__(256, 4) adamw_step8_kernel(const __grid_constant__ AwTable tab, AwLaunch l, const float* __restrict__ coef, int stride, AwStep a) {
   __shared__ __align__(16) char ring[kRing8];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);  // the compiler sees that a warp has one
   const int k = (int)(blockIdx.x / l.units);
   const unsigned q = blockIdx.x - (unsigned)k * l.units;
   const int i = find_tensor(tab.start, l.count, q);

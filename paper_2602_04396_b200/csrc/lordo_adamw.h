@@ -10,7 +10,6 @@ inline long long aw_piece(long long elements) {
   const long long p = (elements / (148 * 8) + 2047) / 2048 * 2048;
   return p < 2048 ? 2048 : p > 32768 ? 32768 : p;
 }
-constexpr int kAwChunk = 32768;  // elements of one worker's tensor behind a partial sum of squares
 constexpr int kAwOuter = 4096;   // elements of a tensor that a CTA of the synchronisation works on
 constexpr int kAwTable = 512;    // tensors of one launch
 
@@ -55,6 +54,7 @@ struct AwLaunch {
 
 struct AwClip {
   double* partial;     // [K][total]
+  int chunk;           // elements of one worker's tensor behind a partial sum
   unsigned total, at;  // chunks of a worker in all launches, and before this one
   unsigned* tickets;   // scope 0: [K]; scope 1: [n_tensors][K]; zero before the first launch, and again after every step
   double rho;

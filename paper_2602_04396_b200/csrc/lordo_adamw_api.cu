@@ -43,7 +43,7 @@ struct lordo_adamw_ctx {
   float* d_coef = nullptr;
   size_t n_tickets = 0;
   unsigned total_chunks = 0;
-  int piece = 0;
+  int piece = 0, chunk = 0;
   int64_t steps = 0, outers = 0, launches = 0;
   std::string err;
 };
@@ -106,6 +106,7 @@ size_t build(lordo_adamw_ctx* c, const lordo_adamw_buffers* buf, char* base) {
   long long elements = 0;
   for (int i = 0; i < nt; ++i) elements += cfg.tensors[i].n * K;
   c->piece = (int)aw_piece(elements);
+  c->chunk = (int)sq_chunk(elements);
   for (int first = 0; first < nt; first += kAwTable) {
     c->groups.emplace_back();
     Group& g = c->groups.back();
@@ -118,7 +119,7 @@ size_t build(lordo_adamw_ctx* c, const lordo_adamw_buffers* buf, char* base) {
       const long long n = cfg.tensors[first + x].n;
       g.norm.start[x] = g.chunks; g.step.start[x] = g.pieces;
       g.outer.push_back(g.blocks);
-      g.chunks += (unsigned)cdiv(n, kAwChunk);
+      g.chunks += (unsigned)cdiv(n, c->chunk);
       g.pieces += (unsigned)cdiv(n, c->piece);
       g.blocks += (unsigned)cdiv(n, kAwOuter);
     }
@@ -216,7 +217,7 @@ int step(lordo_adamw_ctx* c, const lordo_grad* G, double lr, double beta1, doubl
   int stride = 0;
   if (!coef && cfg.clip_rho > 0.0) {
     for (Group& g : c->groups) {
-      const AwClip clip = {c->d_partial, c->total_chunks, g.chunks_before, c->d_tickets, cfg.clip_rho, cfg.clip_scope, cfg.n_tensors, c->d_coef, c->d_status};
+      const AwClip clip = {c->d_partial, c->chunk, c->total_chunks, g.chunks_before, c->d_tickets, cfg.clip_rho, cfg.clip_scope, cfg.n_tensors, c->d_coef, c->d_status};
       launch_aw_norm(launch_of(c, g, g.chunks), g.norm, clip, st);
       c->launches += 1;
     }
