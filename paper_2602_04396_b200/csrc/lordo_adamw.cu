@@ -56,9 +56,13 @@ __device__ __forceinline__ float row_grad(const AwTensor& T, int k, long long e)
   const int2 seg = __ldg(T.segs + (long long)k * (T.n / T.d) + v);
   return seg.x < seg.y ? T.rows[((long long)k * T.cap + seg.x) * T.d + (e - v * T.d)] : 0.f;
 }
+// Row of element e, a multiple of 8, of such a table, whose rows are whole eighths.
+__device__ __forceinline__ unsigned row_of(const AwTensor& T, long long e) {
+  return (unsigned)(((unsigned long long)(unsigned)(e >> 3) * T.row_mul) >> (31 + T.row_shift));
+}
 __device__ __forceinline__ void row_grad8(const AwTensor& T, int k, long long e, float (&g)[8]) {
-  if ((T.d & 7) == 0) {
-    const long long v = e / T.d;
+  if (T.row_mul) {
+    const long long v = row_of(T, e);
     const int2 seg = __ldg(T.segs + (long long)k * (T.n / T.d) + v);
     if (seg.x < seg.y) {
       load8<LORDO_F32>(T.rows, ((long long)k * T.cap + seg.x) * T.d + (e - v * T.d), g);
@@ -396,6 +400,8 @@ struct Arrays8 {  // of one worker
   const void* G;
   void* W;
   unsigned char *m, *v, *ms, *vs;
+  const int2* segs;   // with a gradient by tokens
+  const float* rows;
 };
 
 template <int BYTES>
@@ -436,9 +442,10 @@ __device__ __forceinline__ void put8(char* to, const float2 (&x)[4]) {
 
 // Whole blocks b0 + warp, + 8, ... below b1 (at most 32 of a warp), eight elements a lane, all of it aligned. A lane copies what it will use to its
 // warp's ring in shared memory, some blocks ahead; no other lane touches that.
+// ROWS: the gradient is in rows that were summed by token (fp32); which row a lane wants of a block is looked up a block ahead of the copies.
 constexpr int kRing8 = 48 * 1024;
-template <int WDT, int GDT>
-__device__ __forceinline__ void step8_blocks(const Arrays8& a, const Step8& s, unsigned long long key, long long b0, long long b1, int lane, int warp, char* ring) {
+template <int WDT, int GDT, bool ROWS>
+__device__ __forceinline__ void step8_blocks(const AwTensor& T, const Arrays8& a, const Step8& s, unsigned long long key, long long b0, long long b1, int lane, int warp, char* ring) {
   constexpr int kWb = WDT == LORDO_F32 ? 4 : 2, kGb = GDT == LORDO_F32 ? 4 : 2, kStep = 8 * kAwBlock;  // elements from block to block
   constexpr int kM = 256 * (kWb + kGb), kStage = kM + 512, kStages = kRing8 / 8 / kStage;
   const long long first = b0 + warp;
@@ -451,9 +458,25 @@ __device__ __forceinline__ void step8_blocks(const Arrays8& a, const Step8& s, u
   char* pw = reinterpret_cast<char*>(a.W) + e0 * kWb;
   const char* pg = reinterpret_cast<const char*>(a.G) + e0 * kGb;
   unsigned char *pm = a.m + e0, *pv = a.v + e0;
+  const float* row = nullptr;  // of the next block that is fetched, or null: no token
+  auto look_up = [&](unsigned x) {
+    if (ROWS && x < count) {
+      const long long e = e0 + x * kStep;
+      const unsigned v = row_of(T, e);
+      const int2 seg = __ldg(a.segs + v);
+      row = seg.x < seg.y ? a.rows + (long long)seg.x * T.d + (e - (long long)v * T.d) : nullptr;
+    }
+  };
   auto fetch = [&](unsigned slot) {
     copy8<WDT>(at + slot, pw, 0);
-    copy8<GDT>(at + slot + 256 * kWb, pg, 0);
+    if (!ROWS) {
+      copy8<GDT>(at + slot + 256 * kWb, pg, 0);
+    } else if (row) {
+      copy8<GDT>(at + slot + 256 * kWb, row, 0);
+    } else {
+      float4* p = reinterpret_cast<float4*>(mine + slot + 256 * kWb);
+      p[0] = p[32] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
     copy_async<8>(at + slot + kM - 8 * lane, pm);
     copy_async<8>(at + slot + kM + 256 - 8 * lane, pv);
   };
@@ -463,9 +486,11 @@ __device__ __forceinline__ void step8_blocks(const Arrays8& a, const Step8& s, u
     pm += kStep;
     pv += kStep;
   };
+  look_up(0);
 #pragma unroll
   for (int x = 0; x < kStages - 1; ++x) {
     if (x < count) fetch(x * kStage);
+    look_up(x + 1);
     asm volatile("cp.async.commit_group;" ::: "memory");
     advance();
   }
@@ -473,6 +498,7 @@ __device__ __forceinline__ void step8_blocks(const Arrays8& a, const Step8& s, u
   unsigned slot = 0, into = (kStages - 1) * kStage;
   for (int x = 0; x < count; ++x) {
     if (x + kStages - 1 < count) fetch(into);
+    look_up(x + kStages);
     asm volatile("cp.async.commit_group;\ncp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
     const char* p = mine + slot;
     float2 g[4], w[4];
@@ -526,9 +552,12 @@ __global__ void __launch_bounds__(256, 4) adamw_step8_kernel(const __grid_consta
   x.vs = T.vs + (long long)k * T.nb;
   long long b0 = (long long)(q - tab.start[i]) * (l.piece / kAwBlock);
   const long long b1 = b0 + l.piece / kAwBlock < T.nb ? b0 + l.piece / kAwBlock : T.nb;
-  if (G && (base & 7) == 0) {
+  x.segs = T.segs + (G || !T.d ? 0 : (long long)k * (T.n / T.d));
+  x.rows = T.rows + (long long)k * T.cap * T.d;
+  if ((base & 7) == 0 && (G || T.row_mul)) {
     const long long whole = T.n / kAwBlock < b1 ? T.n / kAwBlock : b1;
-    step8_blocks<WDT, GDT>(x, s, key, b0, whole, lane, warp, ring);
+    if (G) step8_blocks<WDT, GDT, false>(T, x, s, key, b0, whole, lane, warp, ring);
+    else step8_blocks<WDT, LORDO_F32, true>(T, x, s, key, b0, whole, lane, warp, ring);
     b0 = whole > b0 ? whole : b0;
   }
   // the last block of a worker, workers whose arrays begin at odd addresses, gradients by tokens

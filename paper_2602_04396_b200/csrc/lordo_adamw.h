@@ -28,6 +28,9 @@ struct AwTensor {
   const float* rows;       // [K][cap][d] sums, at the first sorted entry of their token
   const double* rowsq;     // [K][rowsq_count] sums of their squares
   const int* rowsq_count;
+  // rows of eighths of d: x / (d / 8) = (x * row_mul) >> (31 + row_shift) for x < 2^31; row_mul = 0 where d is no multiple of 8 or n too large
+  unsigned row_mul;
+  int row_shift;
 };
 
 // Gradients and the dealing of a launch, handed over as kernel arguments: no copy to the device, and nothing that a later call could overwrite.

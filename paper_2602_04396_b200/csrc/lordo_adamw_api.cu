@@ -152,6 +152,11 @@ size_t build(lordo_adamw_ctx* c, const lordo_adamw_buffers* buf, char* base) {
       tb.rows.sq = reinterpret_cast<double*>(take(8 * (size_t)K * tok_row_blocks_max(t.max_tokens, t.row)));
       tb.rows.count = reinterpret_cast<int*>(take(4));
       tb.rows.cap = t.max_tokens;
+      if (t.row % 8 == 0 && t.n / 8 < (1ll << 31)) {  // the multiplier is at most 2^32 - 1, and off by less than 2^row_shift / 2^(31 + row_shift) of the quotient
+        const unsigned long long eighths = (unsigned long long)t.row / 8;
+        while ((1ull << a.row_shift) < eighths) a.row_shift += 1;
+        a.row_mul = (unsigned)((1ull << (31 + a.row_shift)) / eighths + 1);
+      }
       a.segs = tb.scratch.segs; a.rows = tb.rows.rows; a.rowsq = tb.rows.sq; a.rowsq_count = tb.rows.count;
       c->tables.push_back(tb);
     }
@@ -209,9 +214,7 @@ int step(lordo_adamw_ctx* c, const lordo_grad* G, double lr, double beta1, doubl
     const long long d = c->tensors[i].row;
     const TokProblem p = {G[i].tokens, G[i].index == LORDO_I64, cfg.K, c->tensors[i].n / d, G[i].T, d, G[i].G, cfg.g_dtype, G[i].scale};
     const int which = tok_sort(p, tb.scratch, st);
-    tok_chunks(p, tb.scratch, which, st);
-    tok_rows(p, tb.scratch, which, tb.rows, st);
-    c->launches += p.T >= kTokChunk ? 3 : 2;
+    c->launches += 1 + tok_rows(p, tb.scratch, which, tb.rows, st);
   }
   const float* coef = coef_dev;
   int stride = 0;

@@ -135,172 +135,205 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(SortArgs a) {
 // ---------------------------------------------------------------------------------------------
 // Sums. A warp works on 32 * VEC columns of one token's rows.
 // ---------------------------------------------------------------------------------------------
-template <int DT, int VEC>
-__device__ __forceinline__ void add_row(const void* base, long long at, float (&acc)[VEC]) {
-  if constexpr (VEC == 1) {
-    acc[0] += load1(base, DT, at);
-  } else if constexpr (DT == LORDO_F32) {
-    const float4 x = __ldcs(reinterpret_cast<const float4*>(reinterpret_cast<const float*>(base) + at));
-    acc[0] += x.x; acc[1] += x.y; acc[2] += x.z; acc[3] += x.w;
-  } else {
-    const uint4 x = __ldcs(reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned short*>(base) + at));
-    const unsigned r[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      acc[2 * j] += __uint_as_float(r[j] << 16);
-      acc[2 * j + 1] += __uint_as_float(r[j] & 0xFFFF0000u);
-    }
+template <int DT, int VEC>  // VEC consecutive elements as they are stored: 16 bytes, or one
+struct Piece {
+  uint4 r;
+  __device__ __forceinline__ void load(const void* base, long long at) {
+    if constexpr (VEC == 1) r.x = __float_as_uint(load1(base, DT, at));
+    else r = __ldcs(reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(base) + at * (DT == LORDO_F32 ? 4 : 2)));
   }
-}
-
-struct SumArgs {
-  const void* dY;
-  const int2* order;   // [K][cap]
-  const int2* segs;    // [K][V]
-  const int* valid;
-  float* chunks;       // [K][cap / 32][d]
-  long long V, T, cap, d;
-  int groups;          // column groups of a row
-  float scale;
-  void* out;
-  double* sq;          // [K][gridDim.x]
-  int* count;          // gridDim.x
-  long long out_cap;   // rows of a worker in `out` (sums in rows of their own)
-};
-
-// Sum of sorted entries [s, e) of worker k, columns from `col` on. Every lane is here; `on`: it has columns.
-template <int DT, int VEC>
-__device__ __forceinline__ void sum_entries(const SumArgs& a, int k, int s, int e, long long col, bool on, int lane, float (&acc)[VEC]) {
-  const int2* order = a.order + (long long)k * a.cap;
-  const long long first = (long long)k * a.T * a.d + col;
-  for (int b = s; b < e; b += 32) {
-    const int mine = b + lane < e ? __ldcg(order + b + lane).y : 0;
-    const int n = e - b < 32 ? e - b : 32;
-    int j = 0;
-    for (; j + 4 <= n; j += 4) {
-      long long at[4];
+  __device__ __forceinline__ void add_to(float (&acc)[VEC]) const {
+    const unsigned w[4] = {r.x, r.y, r.z, r.w};
+    if constexpr (VEC == 1 || DT == LORDO_F32) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) at[x] = first + (long long)__shfl_sync(0xffffffffu, mine, j + x) * a.d;
-      if (on) {
+      for (int j = 0; j < VEC; ++j) acc[j] += __uint_as_float(w[j & 3]);
+    } else {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) add_row<DT, VEC>(a.dY, at[x], acc);
+      for (int j = 0; j < VEC / 2; ++j) {
+        acc[2 * j] += __uint_as_float(w[j & 3] << 16);
+        acc[2 * j + 1] += __uint_as_float(w[j & 3] & 0xFFFF0000u);
       }
     }
-    for (; j < n; ++j) {
-      const long long at = first + (long long)__shfl_sync(0xffffffffu, mine, j) * a.d;
-      if (on) add_row<DT, VEC>(a.dY, at, acc);
-    }
   }
-}
-
-// Sum of one token's entries: the ends one by one, the whole chunks between them from tok_chunks.
-template <int DT, int VEC>
-__device__ __forceinline__ void sum_segment(const SumArgs& a, int k, int s, int e, long long col, bool on, int lane, float (&acc)[VEC]) {
-  const int c0 = (s + kTokChunk - 1) / kTokChunk, c1 = e / kTokChunk;
-  if (c1 <= c0) {
-    sum_entries<DT, VEC>(a, k, s, e, col, on, lane, acc);
-    return;
-  }
-  sum_entries<DT, VEC>(a, k, s, c0 * kTokChunk, col, on, lane, acc);
-  if (on) {
-    const float* p = a.chunks + ((long long)k * (a.cap / kTokChunk) + c0) * a.d + col;
-    for (int c = c0; c < c1; ++c, p += a.d)
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) acc[j] += __ldcg(p + j);
-  }
-  sum_entries<DT, VEC>(a, k, c1 * kTokChunk, e, col, on, lane, acc);
-}
-
-template <int DT, int VEC>
-__global__ void __launch_bounds__(256) chunk_sums_kernel(SumArgs a) {
-  const int lane = threadIdx.x & 31, k = blockIdx.y;
-  dep_begin();
-  const long long item = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const long long c = item / a.groups;
-  const int s = (int)(c * kTokChunk);
-  if (s + kTokChunk > a.valid[k]) return;
-  const int2* order = a.order + (long long)k * a.cap;
-  if (__ldcg(order + s).x != __ldcg(order + s + kTokChunk - 1).x) return;
-  const long long col = ((item - c * a.groups) * 32 + lane) * VEC;
-  const bool on = col < a.d;
-  float acc[VEC] = {};
-  sum_entries<DT, VEC>(a, k, s, s + kTokChunk, col, on, lane, acc);
-  if (on) {
-    float* p = a.chunks + ((long long)k * (a.cap / kTokChunk) + c) * a.d + col;
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) p[j] = acc[j];
-  }
-}
+};
 
 template <int VEC>
 __device__ __forceinline__ void put(void* base, int dt, long long at, const float (&x)[VEC]) {
   if constexpr (VEC == 1) {
     store1(base, dt, at, x[0]);
+  } else if (VEC == 8 && dt == LORDO_BF16) {
+    uint4 a;
+    a.x = pack_bf16x2(x[0], x[1]); a.y = pack_bf16x2(x[2], x[3]); a.z = pack_bf16x2(x[4 % VEC], x[5 % VEC]); a.w = pack_bf16x2(x[6 % VEC], x[7 % VEC]);
+    *reinterpret_cast<uint4*>(reinterpret_cast<unsigned short*>(base) + at) = a;
   } else {
 #pragma unroll
     for (int j = 0; j < VEC; j += 4) store4(base, dt, at + j, make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]));
   }
 }
 
-constexpr int kSumItems = 4;  // items a warp works on one after another
 enum SumMode { SUM_DENSE = 0, SUM_ADD = 1, SUM_ROWS = 2 };
 
-// DENSE: an item is a row of the table (rows without a token become zero). ADD, ROWS: an item is a sorted entry, and works where a
-// token's entries begin.
-template <int DT, int VEC, int MODE>
-__global__ void __launch_bounds__(256) token_sums_kernel(SumArgs a, int out_dt) {
+struct SumArgs {
+  const void* dY;
+  const int2* order;    // [K][T]
+  const int2* segs;     // [K][V]
+  const int* valid;
+  float* parts;         // [K][windows][2][d]: of the token that came in from the window before, of the one that goes on into the next
+  long long V, T, d;
+  int groups, windows;  // column groups of a row, windows of a worker
+  float scale;
+  void* out;
+  int out_dt;
+  double* sq;           // [K][2 * gridDim.x]
+  int* count;           // 2 * gridDim.x
+  long long out_cap;    // rows of a worker in `out` (sums in rows of their own)
+  unsigned sum_blocks;  // blocks that form sums; the rest write the zeros of rows without a token
+};
+
+// The sum of token v, whose first sorted entry is `start`.
+template <int VEC, int MODE>
+__device__ __forceinline__ void emit(const SumArgs& a, int k, int v, int start, long long col, float (&acc)[VEC], float& sq) {
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) acc[j] *= a.scale;
+  if (MODE == SUM_ROWS) {
+    put<VEC>(a.out, LORDO_F32, ((long long)k * a.out_cap + start) * a.d + col, acc);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sq += acc[j] * acc[j];
+  } else {
+    const long long at = ((long long)k * a.V + v) * a.d + col;
+    if (MODE == SUM_ADD) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) acc[j] += load1(a.out, a.out_dt, at + j);
+    }
+    put<VEC>(a.out, a.out_dt, at, acc);
+  }
+}
+
+// Sums of squares of a block: sq[k][which * gridDim.x + block].
+__device__ __forceinline__ void block_squares(const SumArgs& a, int k, int which, float x) {
   __shared__ double red[8];
+  double s = (double)x;
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.0;
+    for (int w = 0; w < 8; ++w) s += red[w];
+    a.sq[(long long)k * 2 * gridDim.x + which * gridDim.x + blockIdx.x] = s;
+    if (k == 0 && blockIdx.x == 0) *a.count = 2 * (int)gridDim.x;
+  }
+}
+
+// A warp walks a window of W sorted entries, 32 * VEC columns of each row of dY, eight rows under way at a time. Tokens whose entries all lie in
+// the window are done; the first part of one that goes on and the last of one that came in are left for join_sums_kernel.
+constexpr int kAhead = 8;
+template <int DT, int VEC, int MODE, int W>
+__device__ __forceinline__ void window_sums(const SumArgs& a, int k, int w, long long col, int lane, float& sq) {
+  const int valid = a.valid[k], s = w * W;
+  if (s >= valid) return;
+  const int n = valid - s < W ? valid - s : W;
+  const int2* order = a.order + (long long)k * a.T + s;
+  const int2 mine = lane < n ? __ldcg(order + lane) : make_int2(-1, 0);
+  const int before = s > 0 ? __ldcg(order - 1).x : -1, behind = s + n < valid ? __ldcg(order + n).x : -1;
+  int next = __shfl_down_sync(0xffffffffu, mine.x, 1);
+  if (lane == n - 1) next = behind;
+  const unsigned ends = __ballot_sync(0xffffffffu, lane < n && next != mine.x);
+  const bool on = col < a.d;
+  bool came_in = before == __shfl_sync(0xffffffffu, mine.x, 0);
+  int start = s;
+  float acc[VEC] = {};
+  float* part = a.parts + ((long long)k * a.windows + w) * 2 * a.d + col;
+  const long long first = (long long)k * a.T * a.d + (on ? col : 0);
+  for (int b = 0; b < n; b += kAhead) {
+    Piece<DT, VEC> x[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int pos = __shfl_sync(0xffffffffu, mine.y, (b + j) & 31);
+      if (b + j < n && on) x[j].load(a.dY, first + (long long)pos * a.d);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (b + j >= n) break;
+      if (on) x[j].add_to(acc);
+      if ((ends >> (b + j)) & 1u) {
+        const int v = __shfl_sync(0xffffffffu, mine.x, b + j);
+        if (on) {
+          if (came_in) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) part[i] = acc[i];
+          } else {
+            emit<VEC, MODE>(a, k, v, start, col, acc, sq);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
+        came_in = false;
+        start = s + b + j + 1;
+      }
+    }
+  }
+  if (!((ends >> (n - 1)) & 1u) && on) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) part[(came_in ? 0 : a.d) + i] = acc[i];
+  }
+}
+
+template <int DT, int VEC, int MODE, int W>
+__global__ void __launch_bounds__(256) window_sums_kernel(SumArgs a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = blockIdx.y;
   dep_begin();
-  const long long rows = MODE == SUM_DENSE ? a.V : a.valid[k];
-  const long long items = rows * a.groups;
+  if (MODE == SUM_DENSE && blockIdx.x >= a.sum_blocks) {  // 32 rows a warp
+    const long long v0 = ((long long)(blockIdx.x - a.sum_blocks) * 8 + warp) * 32;
+    if (v0 >= a.V) return;
+    const int2 seg = v0 + lane < a.V ? __ldcg(a.segs + (long long)k * a.V + v0 + lane) : make_int2(0, 1);
+    unsigned empty = __ballot_sync(0xffffffffu, seg.x >= seg.y);
+    const float zero[VEC] = {};
+    while (empty) {
+      const int r = __ffs(empty) - 1;
+      empty &= empty - 1;
+      for (long long col = lane * VEC; col < a.d; col += 32 * VEC) put<VEC>(a.out, a.out_dt, ((long long)k * a.V + v0 + r) * a.d + col, zero);
+    }
+    return;
+  }
+  const long long item = (long long)blockIdx.x * 8 + warp;
+  const long long w = item / a.groups;
   float sq = 0.f;
-  for (int x = 0; x < kSumItems; ++x) {
-    const long long item = ((long long)blockIdx.x * kSumItems + x) * 8 + warp;
-    if (item >= items) break;
-    const long long row = item / a.groups;
-    const long long col = ((item - row * a.groups) * 32 + lane) * VEC;
-    const bool on = col < a.d;
-    float acc[VEC] = {};
-    int2 seg;
-    long long v = row;
-    if (MODE == SUM_DENSE) {
-      seg = __ldcg(a.segs + (long long)k * a.V + row);
-    } else {
-      const int2* order = a.order + (long long)k * a.cap;
-      v = __ldcg(order + row).x;
-      if (row > 0 && __ldcg(order + row - 1).x == v) continue;
-      seg = __ldcg(a.segs + (long long)k * a.V + v);
-    }
-    sum_segment<DT, VEC>(a, k, seg.x, seg.y, col, on, lane, acc);
-    if (!on) continue;
+  if (w < a.windows) window_sums<DT, VEC, MODE, W>(a, k, (int)w, ((item - w * a.groups) * 32 + lane) * VEC, lane, sq);
+  if (MODE == SUM_ROWS) block_squares(a, k, 0, sq);
+}
+
+// Tokens whose entries begin in one window and go on in others: their parts in the order of the windows.
+template <int VEC, int MODE, int W>
+__global__ void __launch_bounds__(256) join_sums_kernel(SumArgs a) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = blockIdx.y;
+  dep_begin();
+  const long long item = (long long)blockIdx.x * 8 + warp;
+  const int w = (int)(item / a.groups);
+  const long long col = ((item - (long long)w * a.groups) * 32 + lane) * VEC;
+  const int valid = a.valid[k], last = (w + 1) * W - 1;
+  float sq = 0.f;
+  if (w < a.windows && last + 1 < valid) {
+    const int2* order = a.order + (long long)k * a.T;
+    const int v = __ldcg(order + last).x;
+    if (v == __ldcg(order + last + 1).x) {
+      const int2 seg = __ldcg(a.segs + (long long)k * a.V + v);
+      if (seg.x >= w * W && col < a.d) {  // it begins here
+        const float* p = a.parts + ((long long)k * a.windows + w) * 2 * a.d + a.d + col;
+        float acc[VEC];
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) acc[j] *= a.scale;
-    if (MODE == SUM_ROWS) {
-      put<VEC>(a.out, LORDO_F32, ((long long)k * a.out_cap + row) * a.d + col, acc);
+        for (int i = 0; i < VEC; ++i) acc[i] = __ldcg(p + i);
+        const int end = (seg.y - 1) / W;
+        p += a.d;
+#pragma unroll 4
+        for (int x = w + 1; x <= end; ++x, p += 2 * a.d) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) sq += acc[j] * acc[j];
-    } else {
-      const long long at = ((long long)k * a.V + v) * a.d + col;
-      if (MODE == SUM_ADD) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) acc[j] += load1(a.out, out_dt, at + j);
+          for (int i = 0; i < VEC; ++i) acc[i] += __ldcg(p + i);
+        }
+        emit<VEC, MODE>(a, k, v, seg.x, col, acc, sq);
       }
-      put<VEC>(a.out, out_dt, at, acc);
     }
   }
-  if (MODE == SUM_ROWS) {
-    double s = (double)sq;
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (lane == 0) red[warp] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      s = 0.0;
-      for (int x = 0; x < 8; ++x) s += red[x];
-      a.sq[(long long)k * gridDim.x + blockIdx.x] = s;
-      if (k == 0 && blockIdx.x == 0) *a.count = (int)gridDim.x;
-    }
-  }
+  if (MODE == SUM_ROWS) block_squares(a, k, 1, sq);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -311,14 +344,16 @@ __global__ void __launch_bounds__(256) lookup_kernel(const void* __restrict__ W,
                                                      long long T, long long pieces, float scale, void* __restrict__ out, int out_dt) {
   dep_begin();
   const long long per_row = (d + VEC - 1) / VEC;
-  const long long p = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (p >= pieces) return;
-  const long long row = p / per_row, col = (p - row * per_row) * VEC;
+  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (at >= pieces) return;
+  const long long row = at / per_row, col = (at - row * per_row) * VEC;
   const long long v = is64 ? reinterpret_cast<const long long*>(tokens)[row] : (long long)reinterpret_cast<const int*>(tokens)[row];
   const long long k = row / T;
   float x[VEC] = {};
   if (v >= 0 && v < V) {
-    add_row<DT, VEC>(W, (k * V + v) * d + col, x);
+    Piece<DT, VEC> p;
+    p.load(W, (k * V + v) * d + col);
+    p.add_to(x);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) x[j] *= scale;
   }
@@ -333,36 +368,45 @@ int token_bits(long long V) {  // of the largest key, V
 
 bool wide(const void* p, long long d, int dt) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && d % (dt == LORDO_F32 ? 4 : 8) == 0; }
 
-SumArgs sum_args(const TokProblem& p, const TokScratch& s, int which, int vec) {
-  SumArgs a = {};
-  a.dY = p.dY; a.order = s.buf[which]; a.segs = s.segs; a.valid = s.valid; a.chunks = s.chunks;
-  a.V = p.V; a.T = p.T; a.d = p.d; a.scale = p.scale;
-  a.cap = p.T;
-  a.groups = (int)((p.d + 32 * vec - 1) / (32 * vec));
-  return a;
-}
-
-template <int MODE>
-void run_sums(SumArgs a, const TokProblem& p, int out_dt, unsigned blocks, int vec, cudaStream_t st) {
-  const dim3 grid(blocks, p.K);
-  if (p.y_dt == LORDO_F32) {
-    if (vec == 4) launch_dep(token_sums_kernel<LORDO_F32, 4, MODE>, grid, 256, 0, st, a, out_dt);
-    else launch_dep(token_sums_kernel<LORDO_F32, 1, MODE>, grid, 256, 0, st, a, out_dt);
-  } else {
-    if (vec == 8) launch_dep(token_sums_kernel<LORDO_BF16, 8, MODE>, grid, 256, 0, st, a, out_dt);
-    else launch_dep(token_sums_kernel<LORDO_BF16, 1, MODE>, grid, 256, 0, st, a, out_dt);
-  }
-}
-
 // Columns of a lane: 16 bytes of dY where rows and arrays allow it.
-int sum_vec(const TokProblem& p, const void* out, int out_dt) {
+int sum_vec(const TokProblem& p, const void* out) {
   const int vec = p.y_dt == LORDO_F32 ? 4 : 8;
   return p.d % vec == 0 && wide(p.dY, p.d, p.y_dt) && (reinterpret_cast<uintptr_t>(out) & 15u) == 0 ? vec : 1;
 }
 
-unsigned sum_blocks(long long rows, long long d, int vec) {
-  const long long items = rows * ((d + 32 * vec - 1) / (32 * vec));
-  return items > 0 ? (unsigned)((items + 8 * kSumItems - 1) / (8 * kSumItems)) : 1u;
+// Sorted entries of a window.
+constexpr int kWindow = 32;
+int windows_of(long long T) { return (int)((T + kWindow - 1) / kWindow); }
+
+unsigned sum_blocks(long long T, long long d, int vec) {
+  const long long items = windows_of(T) * ((d + 32 * vec - 1) / (32 * vec));
+  return items > 0 ? (unsigned)((items + 7) / 8) : 1u;
+}
+
+template <int MODE>
+int run_sums(const TokProblem& p, const TokScratch& s, int which, void* out, int out_dt, const TokRows* r, cudaStream_t st) {
+  const int vec = sum_vec(p, out);
+  SumArgs a = {};
+  a.dY = p.dY; a.order = s.buf[which]; a.segs = s.segs; a.valid = s.valid; a.parts = s.parts;
+  a.V = p.V; a.T = p.T; a.d = p.d; a.scale = p.scale;
+  a.groups = (int)((p.d + 32 * vec - 1) / (32 * vec));
+  a.windows = windows_of(p.T);
+  a.out = out; a.out_dt = out_dt;
+  if (r) { a.sq = r->sq; a.count = r->count; a.out_cap = r->cap; }
+  a.sum_blocks = sum_blocks(p.T, p.d, vec);
+  const unsigned zeros = MODE == SUM_DENSE ? (unsigned)((p.V + 255) / 256) : 0u;
+  const dim3 grid(a.sum_blocks + zeros, p.K), join(a.sum_blocks, p.K);
+  if (p.y_dt == LORDO_F32) {
+    if (vec == 4) launch_dep(window_sums_kernel<LORDO_F32, 4, MODE, kWindow>, grid, 256, 0, st, a);
+    else launch_dep(window_sums_kernel<LORDO_F32, 1, MODE, kWindow>, grid, 256, 0, st, a);
+  } else {
+    if (vec == 8) launch_dep(window_sums_kernel<LORDO_BF16, 8, MODE, kWindow>, grid, 256, 0, st, a);
+    else launch_dep(window_sums_kernel<LORDO_BF16, 1, MODE, kWindow>, grid, 256, 0, st, a);
+  }
+  if (vec == 8) launch_dep(join_sums_kernel<8, MODE, kWindow>, join, 256, 0, st, a);
+  else if (vec == 4) launch_dep(join_sums_kernel<4, MODE, kWindow>, join, 256, 0, st, a);
+  else launch_dep(join_sums_kernel<1, MODE, kWindow>, join, 256, 0, st, a);
+  return 2;
 }
 
 }  // namespace
@@ -379,7 +423,7 @@ TokScratch tok_scratch(char* base, int K, long long V, long long d, long long ca
   s.buf[1] = reinterpret_cast<int2*>(take(8ll * K * cap));
   s.segs = reinterpret_cast<int2*>(take(8ll * K * V));
   s.valid = reinterpret_cast<int*>(take(4ll * K));
-  s.chunks = reinterpret_cast<float*>(take(4ll * K * (cap / kTokChunk) * d));
+  s.parts = reinterpret_cast<float*>(take(8ll * K * windows_of(cap) * d));
   s.bytes = off;
   return s;
 }
@@ -407,35 +451,14 @@ int tok_sort(const TokProblem& p, const TokScratch& s, cudaStream_t st) {
   return (a.passes - 1) & 1;
 }
 
-void tok_chunks(const TokProblem& p, const TokScratch& s, int which, cudaStream_t st) {
-  if (p.T < kTokChunk) return;
-  const int vec = sum_vec(p, s.chunks, LORDO_F32);
-  const SumArgs a = sum_args(p, s, which, vec);
-  const dim3 grid((unsigned)((p.T / kTokChunk * a.groups + 7) / 8), p.K);
-  if (p.y_dt == LORDO_F32) {
-    if (vec == 4) launch_dep(chunk_sums_kernel<LORDO_F32, 4>, grid, 256, 0, st, a);
-    else launch_dep(chunk_sums_kernel<LORDO_F32, 1>, grid, 256, 0, st, a);
-  } else {
-    if (vec == 8) launch_dep(chunk_sums_kernel<LORDO_BF16, 8>, grid, 256, 0, st, a);
-    else launch_dep(chunk_sums_kernel<LORDO_BF16, 1>, grid, 256, 0, st, a);
-  }
+int tok_dense(const TokProblem& p, const TokScratch& s, int which, void* dW, int w_dt, int accumulate, cudaStream_t st) {
+  return accumulate ? run_sums<SUM_ADD>(p, s, which, dW, w_dt, nullptr, st) : run_sums<SUM_DENSE>(p, s, which, dW, w_dt, nullptr, st);
 }
 
-void tok_dense(const TokProblem& p, const TokScratch& s, int which, void* dW, int w_dt, int accumulate, cudaStream_t st) {
-  const int vec = sum_vec(p, dW, w_dt);
-  SumArgs a = sum_args(p, s, which, vec);
-  a.out = dW;
-  if (accumulate) run_sums<SUM_ADD>(a, p, w_dt, sum_blocks(p.T, p.d, vec), vec, st);
-  else run_sums<SUM_DENSE>(a, p, w_dt, sum_blocks(p.V, p.d, vec), vec, st);
-}
+long long tok_row_blocks_max(long long cap, long long d) { return 2ll * sum_blocks(cap, d, 1); }
 
-long long tok_row_blocks_max(long long cap, long long d) { return sum_blocks(cap, d, 1); }
-
-void tok_rows(const TokProblem& p, const TokScratch& s, int which, const TokRows& r, cudaStream_t st) {
-  const int vec = sum_vec(p, r.rows, LORDO_F32);
-  SumArgs a = sum_args(p, s, which, vec);
-  a.out = r.rows; a.sq = r.sq; a.count = r.count; a.out_cap = r.cap;
-  run_sums<SUM_ROWS>(a, p, LORDO_F32, sum_blocks(p.T, p.d, vec), vec, st);
+int tok_rows(const TokProblem& p, const TokScratch& s, int which, const TokRows& r, cudaStream_t st) {
+  return run_sums<SUM_ROWS>(p, s, which, r.rows, LORDO_F32, &r, st);
 }
 
 }  // namespace lordo
@@ -514,7 +537,6 @@ int lordo_embedding_grad(const void* dY, int y_dtype, const void* tokens, int in
   if (cudaPeekAtLastError() != cudaSuccess) return LORDO_ERR_CUDA;
   TokProblem p = {tokens, index == LORDO_I64, K, V, T, d, dY, y_dtype, scale};
   const int which = tok_sort(p, s, st);
-  tok_chunks(p, s, which, st);
   tok_dense(p, s, which, dW, w_dtype, accumulate, st);
   return cudaPeekAtLastError() == cudaSuccess ? LORDO_OK : LORDO_ERR_CUDA;
 }

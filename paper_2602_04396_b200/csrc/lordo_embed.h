@@ -5,18 +5,16 @@
 
 namespace lordo {
 
-constexpr int kTokChunk = 32;  // sorted entries whose sum is formed on its own where they all belong to one token
-
 // Scratch of one table: K workers with up to `cap` tokens each.
 struct TokScratch {
   int2* buf[2];     // [K][cap] (token, position), by turns
   int2* segs;       // [K][V] first and last + 1 sorted entry of every token, 0 0 without one
   int* valid;       // [K] tokens inside [0, V)
-  float* chunks;    // [K][cap / 32][d] sums of chunks that belong to one token
+  float* parts;     // [K][windows][2][d] sums of tokens whose entries lie in more than one window
   long long bytes;
 };
 
-// With base null only measures. The same for every T <= cap.
+// With base null only measures. Good for every T <= cap.
 TokScratch tok_scratch(char* base, int K, long long V, long long d, long long cap);
 
 struct TokProblem {
@@ -31,12 +29,10 @@ struct TokProblem {
 
 // Sorts every worker's tokens, ties by position; returns the buffer (0 or 1) that holds the order.
 int tok_sort(const TokProblem& p, const TokScratch& s, cudaStream_t st);
-// Sums of whole chunks of one token each (after tok_sort, before either of the next two).
-void tok_chunks(const TokProblem& p, const TokScratch& s, int which, cudaStream_t st);
-// dW[k][v] (in w_dt) = the sums, or += for the tokens that occur.
-void tok_dense(const TokProblem& p, const TokScratch& s, int which, void* dW, int w_dt, int accumulate, cudaStream_t st);
-// rows[k][i] (fp32, [K][cap][d]) = the sum of the token whose first sorted entry is i; sq[k][0 .. *count) = sums of their squares,
-// *count at most tok_row_blocks_max.
+// After tok_sort: dW[k][v] (in w_dt) = the sums, or += for the tokens that occur. Returns the launches.
+int tok_dense(const TokProblem& p, const TokScratch& s, int which, void* dW, int w_dt, int accumulate, cudaStream_t st);
+// After tok_sort: rows[k][i] (fp32, [K][cap][d]) = the sum of the token whose first sorted entry is i; sq[k][0 .. *count) = sums of their
+// squares, *count at most tok_row_blocks_max.
 struct TokRows {
   float* rows;
   double* sq;
@@ -44,7 +40,7 @@ struct TokRows {
   long long cap;
 };
 long long tok_row_blocks_max(long long cap, long long d);
-void tok_rows(const TokProblem& p, const TokScratch& s, int which, const TokRows& r, cudaStream_t st);
+int tok_rows(const TokProblem& p, const TokScratch& s, int which, const TokRows& r, cudaStream_t st);
 
 // Argument checks: lordo_status. Limits are what the kernels' grids and 32-bit positions take.
 int check_tokens(int K, int64_t V, int64_t d, int64_t T, int index);
