@@ -213,8 +213,7 @@ int step(lordo_adamw_ctx* c, const lordo_grad* G, double lr, double beta1, doubl
     const Table& tb = c->tables[c->table_of[i]];
     const long long d = c->tensors[i].row;
     const TokProblem p = {G[i].tokens, G[i].index == LORDO_I64, cfg.K, c->tensors[i].n / d, G[i].T, d, G[i].G, cfg.g_dtype, G[i].scale};
-    const int which = tok_sort(p, tb.scratch, st);
-    c->launches += 1 + tok_rows(p, tb.scratch, which, tb.rows, st);
+    c->launches += tok_rows(p, tb.scratch, tb.rows, st);
   }
   const float* coef = coef_dev;
   int stride = 0;

@@ -2,6 +2,9 @@
 //   out[k][t] = scale * W[k][tok[k][t]]           dW[k][v] = scale * sum over t with tok[k][t] = v of dY[k][t]
 // for K workers, each with a table and tokens of its own. Sums are fp32, in the order of the positions, the same on every run.
 #include "lordo_embed.h"
+
+#include <algorithm>
+
 #include "lordo_kernels.h"
 
 namespace lordo {
@@ -9,14 +12,39 @@ namespace {
 
 constexpr int kSortThreads = 1024, kSortWarps = 32, kMaxDigit = 256;
 
+// Rows [first, last) of every worker's table, for the zeros of rows without a token.
+struct Zeros {
+  void* W;
+  long long V, d, first, last;
+  int dt;
+};
+
 struct SortArgs {
   const void* tokens;
   int is64, K, bits, passes;
-  long long T, cap, V;
+  long long T, V;
   int2 *buf0, *buf1, *segs;
   int* valid;
-  int per_warp;  // consecutive positions of a warp, a multiple of 32
+  int per_warp;       // consecutive positions of a warp, a multiple of 32
+  unsigned clusters;  // of the sort; the blocks behind them write zeros
+  Zeros zeros;        // rows that are zeroed whether they have a token or not, before any sum is written
 };
+
+// One of `blocks` blocks writes its share of the rows, whole.
+__device__ __forceinline__ void fill_zeros(const Zeros& z, int K, unsigned block, unsigned blocks) {
+  const long long bytes = z.dt == LORDO_F32 ? 4 : 2, per = (z.last - z.first) * z.d * bytes, stride = z.V * z.d * bytes;
+  char* base = reinterpret_cast<char*>(z.W) + z.first * z.d * bytes;
+  const bool wide = ((reinterpret_cast<unsigned long long>(base) | per | stride) & 15) == 0;
+  const long long unit = wide ? 16 : bytes, units = per / unit;
+  for (int k = 0; k < K; ++k) {
+    char* p = base + k * stride;
+    for (long long x = (long long)block * blockDim.x + threadIdx.x; x < units; x += (long long)blocks * blockDim.x) {
+      if (wide) reinterpret_cast<uint4*>(p)[x] = make_uint4(0u, 0u, 0u, 0u);
+      else if (bytes == 4) reinterpret_cast<unsigned*>(p)[x] = 0u;
+      else reinterpret_cast<unsigned short*>(p)[x] = 0;
+    }
+  }
+}
 
 __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -40,6 +68,10 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(SortArgs a) {
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(C));
   const int k = blockIdx.x / C;
   dep_begin();
+  if (blockIdx.x >= a.clusters * C) {
+    fill_zeros(a.zeros, a.K, blockIdx.x - a.clusters * C, gridDim.x - a.clusters * C);
+    return;
+  }
   if (a.T == 0 && c == 0 && t == 0) a.valid[k] = 0;
   int2* segs = a.segs + (long long)k * a.V;
   for (long long v = c * kSortThreads + t; v < a.V; v += (long long)C * kSortThreads) segs[v] = make_int2(0, 0);
@@ -47,8 +79,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(SortArgs a) {
   const long long end = begin + a.per_warp < a.T ? begin + a.per_warp : a.T;
   const int R = 1 << a.bits;
   const int2* src = nullptr;
-  int2* dst = a.buf0 + (long long)k * a.cap;
-  int2* other = a.buf1 + (long long)k * a.cap;
+  int2* dst = a.buf0 + (long long)k * a.T;
+  int2* other = a.buf1 + (long long)k * a.T;
   auto fetch = [&](long long i) {
     if (src) return __ldcg(src + i);
     const long long at = (long long)k * a.T + i;
@@ -132,6 +164,127 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(SortArgs a) {
   }
 }
 
+// The same where a CTA has at most 1024 * NB positions: a thread keeps its NB pairs in registers, a pass hands them to the thread that owns their place
+// by way of that CTA's shared memory, and only the last one writes to global memory. Counts of a digit lie warp by warp, a warp scans eight
+// digits. Bound by latency: 16384 tokens for each of eight workers, two passes, 21 us by way of L2 with two walks over the keys a pass.
+template <int NB>
+__global__ void __launch_bounds__(kSortThreads) sort_small_kernel(SortArgs a) {
+  __shared__ unsigned short cnt[kMaxDigit][kSortWarps + 2];
+  __shared__ int tot[kMaxDigit], base[kMaxDigit], wsum[8];
+  __shared__ int2 buf[kSortThreads * NB];
+  constexpr int L = kSortThreads * NB;
+  const int t = threadIdx.x, lane = t & 31, w = t >> 5;
+  unsigned c, C;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(c));
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(C));
+  const int k = blockIdx.x / C;
+  dep_begin();
+  if (blockIdx.x >= a.clusters * C) {  // a whole cluster
+    fill_zeros(a.zeros, a.K, blockIdx.x - a.clusters * C, gridDim.x - a.clusters * C);
+    return;
+  }
+  const int T = (int)a.T, V = (int)a.V, begin = (int)c * L + w * (32 * NB) + lane;
+  int2 e[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int i = begin + 32 * b;
+    e[b] = make_int2(-1, i);
+    if (i < T) {
+      const long long at = (long long)k * T + i;
+      const long long v = a.is64 ? reinterpret_cast<const long long*>(a.tokens)[at] : (long long)reinterpret_cast<const int*>(a.tokens)[at];
+      e[b].x = v >= 0 && v < V ? (int)v : V;
+    }
+  }
+  int2* segs = a.segs + (long long)k * V;
+  for (int v = (int)c * kSortThreads + t; v < V; v += (int)C * kSortThreads) segs[v] = make_int2(0, 0);
+  const int R = 1 << a.bits;
+  int2* out = ((a.passes - 1) & 1 ? a.buf1 : a.buf0) + (long long)k * T;
+  for (int p = 0; p < a.passes; ++p) {
+    const int shift = p * a.bits;
+    for (int i = t; i < R * (kSortWarps + 2) / 2; i += kSortThreads) reinterpret_cast<unsigned*>(cnt)[i] = 0u;
+    __syncthreads();
+    int rank[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const bool in = begin + 32 * b < T;
+      const int digit = in ? (e[b].x >> shift) & (R - 1) : -1;
+      const unsigned same = __match_any_sync(0xffffffffu, digit);
+      rank[b] = in ? cnt[digit][w] + __popc(same & ((1u << lane) - 1u)) : 0;
+      __syncwarp();
+      if (in && lane == __ffs(same) - 1) cnt[digit][w] += (unsigned short)__popc(same);
+      __syncwarp();
+    }
+    __syncthreads();
+    for (int x = w; x < R; x += kSortWarps) {
+      const int n = cnt[x][lane];
+      int scan = n;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, scan, o);
+        if (lane >= o) scan += up;
+      }
+      cnt[x][lane] = (unsigned short)(scan - n);
+      if (lane == 31) tot[x] = scan;
+    }
+    if (C > 1) cluster_sync_all(); else __syncthreads();
+    int all = 0, before = 0;
+    if (t < R) {
+      for (unsigned r = 0; r < C; ++r) {
+        const int n = cluster_load(tot + t, r);
+        all += n;
+        if (r < c) before += n;
+      }
+    }
+    int scan = all;
+    if (t < kMaxDigit) {
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, scan, o);
+        if (lane >= o) scan += up;
+      }
+      if (lane == 31) wsum[w] = scan;
+    }
+    __syncthreads();
+    if (t < R) {
+      int first = scan - all + before;
+      for (int x = 0; x < w; ++x) first += wsum[x];
+      base[t] = first;
+    }
+    __syncthreads();
+    const bool last = p + 1 == a.passes;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      if (begin + 32 * b >= T) continue;
+      const int digit = (e[b].x >> shift) & (R - 1);
+      const int at = base[digit] + cnt[digit][w] + rank[b];
+      unsigned to = (unsigned)__cvta_generic_to_shared(buf + at % L);
+      asm volatile("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(to) : "r"(at / L));
+      asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(to), "r"(e[b].x), "r"(e[b].y) : "memory");
+      if (last) out[at] = e[b];
+    }
+    if (C > 1) cluster_sync_all(); else __syncthreads();  // all pairs are in place, and every CTA has read the totals
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+      if (begin + 32 * b < T) e[b] = buf[w * (32 * NB) + lane + 32 * b];
+  }
+  auto token_at = [&](int i) {  // of the order, in whichever CTA's shared memory
+    return i < 0 || i >= T ? -1 : cluster_load(&buf[i % L].x, (unsigned)(i / L));
+  };
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int i = begin + 32 * b;
+    if (i >= T) continue;
+    const int v = e[b].x, prev = token_at(i - 1), next = token_at(i + 1);
+    if (v < V) {
+      if (prev != v) segs[v].x = i;
+      if (next != v) segs[v].y = i + 1;
+      if (next < 0 || next >= V) a.valid[k] = i + 1;
+    } else if (i == 0) {
+      a.valid[k] = 0;
+    }
+  }
+  if (T == 0 && c == 0 && t == 0) a.valid[k] = 0;
+  if (C > 1) cluster_sync_all();  // the others may still read this CTA's shared memory
+}
+
 // ---------------------------------------------------------------------------------------------
 // Sums. A warp works on 32 * VEC columns of one token's rows.
 // ---------------------------------------------------------------------------------------------
@@ -187,7 +340,8 @@ struct SumArgs {
   double* sq;           // [K][2 * gridDim.x]
   int* count;           // 2 * gridDim.x
   long long out_cap;    // rows of a worker in `out` (sums in rows of their own)
-  unsigned sum_blocks;  // blocks that form sums; the rest write the zeros of rows without a token
+  unsigned sum_blocks;  // blocks that form sums; the rest write the zeros of rows without a token,
+  long long zero0, zero1, zero2;  // [zero0, zero1) beside the windows, [zero1, zero2) beside the joining
 };
 
 // The sum of token v, whose first sorted entry is `start`.
@@ -278,21 +432,26 @@ __device__ __forceinline__ void window_sums(const SumArgs& a, int k, int w, long
   }
 }
 
+// Zeros of those rows from v0 to v1 that have no token, 32 rows a warp.
+template <int VEC>
+__device__ __forceinline__ void empty_rows(const SumArgs& a, int k, long long v0, long long v1, int lane) {
+  if (v0 >= v1) return;
+  const int2 seg = v0 + lane < v1 ? __ldcg(a.segs + (long long)k * a.V + v0 + lane) : make_int2(0, 1);
+  unsigned empty = __ballot_sync(0xffffffffu, seg.x >= seg.y);
+  const float zero[VEC] = {};
+  while (empty) {
+    const int r = __ffs(empty) - 1;
+    empty &= empty - 1;
+    for (long long col = lane * VEC; col < a.d; col += 32 * VEC) put<VEC>(a.out, a.out_dt, ((long long)k * a.V + v0 + r) * a.d + col, zero);
+  }
+}
+
 template <int DT, int VEC, int MODE, int W>
 __global__ void __launch_bounds__(256) window_sums_kernel(SumArgs a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = blockIdx.y;
   dep_begin();
-  if (MODE == SUM_DENSE && blockIdx.x >= a.sum_blocks) {  // 32 rows a warp
-    const long long v0 = ((long long)(blockIdx.x - a.sum_blocks) * 8 + warp) * 32;
-    if (v0 >= a.V) return;
-    const int2 seg = v0 + lane < a.V ? __ldcg(a.segs + (long long)k * a.V + v0 + lane) : make_int2(0, 1);
-    unsigned empty = __ballot_sync(0xffffffffu, seg.x >= seg.y);
-    const float zero[VEC] = {};
-    while (empty) {
-      const int r = __ffs(empty) - 1;
-      empty &= empty - 1;
-      for (long long col = lane * VEC; col < a.d; col += 32 * VEC) put<VEC>(a.out, a.out_dt, ((long long)k * a.V + v0 + r) * a.d + col, zero);
-    }
+  if (MODE == SUM_DENSE && blockIdx.x >= a.sum_blocks) {
+    empty_rows<VEC>(a, k, a.zero0 + ((long long)(blockIdx.x - a.sum_blocks) * 8 + warp) * 32, a.zero1, lane);
     return;
   }
   const long long item = (long long)blockIdx.x * 8 + warp;
@@ -307,6 +466,10 @@ template <int VEC, int MODE, int W>
 __global__ void __launch_bounds__(256) join_sums_kernel(SumArgs a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = blockIdx.y;
   dep_begin();
+  if (MODE == SUM_DENSE && blockIdx.x >= a.sum_blocks) {
+    empty_rows<VEC>(a, k, a.zero1 + ((long long)(blockIdx.x - a.sum_blocks) * 8 + warp) * 32, a.zero2, lane);
+    return;
+  }
   const long long item = (long long)blockIdx.x * 8 + warp;
   const int w = (int)(item / a.groups);
   const long long col = ((item - (long long)w * a.groups) * 32 + lane) * VEC;
@@ -324,10 +487,17 @@ __global__ void __launch_bounds__(256) join_sums_kernel(SumArgs a) {
         for (int i = 0; i < VEC; ++i) acc[i] = __ldcg(p + i);
         const int end = (seg.y - 1) / W;
         p += a.d;
-#pragma unroll 4
-        for (int x = w + 1; x <= end; ++x, p += 2 * a.d) {
+        constexpr int kParts = 64 / VEC < 16 ? 64 / VEC : 16;  // under way together
+        for (int x = w + 1; x <= end; x += kParts) {
+          float y[kParts][VEC];
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) acc[i] += __ldcg(p + i);
+          for (int j = 0; j < kParts; ++j, p += 2 * a.d)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) y[j][i] = x + j <= end ? __ldcg(p + i) : 0.f;
+#pragma unroll
+          for (int j = 0; j < kParts; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) acc[i] += y[j][i];
         }
         emit<VEC, MODE>(a, k, v, seg.x, col, acc, sq);
       }
@@ -337,27 +507,43 @@ __global__ void __launch_bounds__(256) join_sums_kernel(SumArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// Lookup
+// Lookup. A warp has kLookRows consecutive rows of the output, 32 * VEC columns of each: their tokens are one load, and the rows of the table
+// are under way together.
 // ---------------------------------------------------------------------------------------------
+constexpr int kLookRows = 8;
 template <int DT, int VEC>
 __global__ void __launch_bounds__(256) lookup_kernel(const void* __restrict__ W, const void* __restrict__ tokens, int is64, long long V, long long d,
-                                                     long long T, long long pieces, float scale, void* __restrict__ out, int out_dt) {
+                                                     long long T, long long rows, int groups, float scale, void* __restrict__ out, int out_dt) {
+  const int lane = threadIdx.x & 31;
   dep_begin();
-  const long long per_row = (d + VEC - 1) / VEC;
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (at >= pieces) return;
-  const long long row = at / per_row, col = (at - row * per_row) * VEC;
-  const long long v = is64 ? reinterpret_cast<const long long*>(tokens)[row] : (long long)reinterpret_cast<const int*>(tokens)[row];
-  const long long k = row / T;
-  float x[VEC] = {};
-  if (v >= 0 && v < V) {
-    Piece<DT, VEC> p;
-    p.load(W, (k * V + v) * d + col);
-    p.add_to(x);
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) x[j] *= scale;
+  const long long item = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const long long first = item / groups * kLookRows;
+  if (first >= rows) return;
+  const int n = rows - first < kLookRows ? (int)(rows - first) : kLookRows;
+  long long mine = -1;  // row of all workers' tables, or none
+  if (lane < n) {
+    const long long at = first + lane;
+    const long long v = is64 ? reinterpret_cast<const long long*>(tokens)[at] : (long long)reinterpret_cast<const int*>(tokens)[at];
+    if (v >= 0 && v < V) mine = at / T * V + v;
   }
-  put<VEC>(out, out_dt, row * d + col, x);
+  const long long col = (item % groups * 32 + lane) * VEC;
+  const bool on = col < d;
+  Piece<DT, VEC> x[kLookRows];
+#pragma unroll
+  for (int j = 0; j < kLookRows; ++j) {
+    const long long row = __shfl_sync(0xffffffffu, mine, j);
+    x[j].r = make_uint4(0u, 0u, 0u, 0u);
+    if (on && row >= 0) x[j].load(W, row * d + col);
+  }
+#pragma unroll
+  for (int j = 0; j < kLookRows; ++j) {
+    if (!on || j >= n) break;
+    float y[VEC] = {};
+    x[j].add_to(y);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) y[i] *= scale;
+    put<VEC>(out, out_dt, (first + j) * d + col, y);
+  }
 }
 
 int token_bits(long long V) {  // of the largest key, V
@@ -383,10 +569,51 @@ unsigned sum_blocks(long long T, long long d, int vec) {
   return items > 0 ? (unsigned)((items + 7) / 8) : 1u;
 }
 
+// Which rows' zeros are written when. While tokens are sorted the memory is idle, so a first part of the table is zeroed then without
+// knowing which rows will have a token; as much more as the joining takes is left to it. What is left is written beside the windows. (All of it
+// there: 50304 x 768, K = 8, 16384 tokens 188 us.)
+constexpr long long kSortBytes = 64ll << 20, kJoinBytes = 64ll << 20;
+
+int sort(const TokProblem& p, const TokScratch& s, const Zeros& zeros, cudaStream_t st) {
+  const int bits = token_bits(p.V);
+  SortArgs a = {};
+  a.tokens = p.tokens; a.is64 = p.is64; a.K = p.K; a.T = p.T; a.V = p.V;
+  a.passes = (bits + 7) / 8;
+  a.bits = (bits + a.passes - 1) / a.passes;
+  a.buf0 = s.buf[0]; a.buf1 = s.buf[1]; a.segs = s.segs; a.valid = s.valid;
+  a.zeros = zeros;
+  int C = 1;
+  while (C < 8 && p.T > 1024ll * C) C *= 2;
+  const long long warps = (long long)C * kSortWarps;
+  a.per_warp = (int)(((p.T + warps - 1) / warps + 31) / 32 * 32);
+  a.clusters = (unsigned)p.K;
+  const unsigned fill = zeros.last > zeros.first ? (unsigned)((128 + C - 1) / C * C) : 0u;
+  cudaLaunchConfig_t lc = {};
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = C; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  lc.gridDim = dim3(C * p.K + fill); lc.blockDim = dim3(kSortThreads); lc.stream = st;
+  lc.attrs = at; lc.numAttrs = 2;
+  if (a.per_warp <= 32) cudaLaunchKernelEx(&lc, sort_small_kernel<1>, a);
+  else if (a.per_warp <= 64) cudaLaunchKernelEx(&lc, sort_small_kernel<2>, a);
+  else if (a.per_warp <= 96) cudaLaunchKernelEx(&lc, sort_small_kernel<3>, a);
+  else cudaLaunchKernelEx(&lc, sort_tokens_kernel, a);
+  return (a.passes - 1) & 1;
+}
+
 template <int MODE>
-int run_sums(const TokProblem& p, const TokScratch& s, int which, void* out, int out_dt, const TokRows* r, cudaStream_t st) {
+int run_sums(const TokProblem& p, const TokScratch& s, void* out, int out_dt, const TokRows* r, cudaStream_t st) {
   const int vec = sum_vec(p, out);
   SumArgs a = {};
+  a.zero0 = a.zero1 = a.zero2 = p.V;
+  if (MODE == SUM_DENSE) {
+    const long long row = p.K * p.d * (out_dt == LORDO_F32 ? 4 : 2);
+    a.zero0 = std::min((long long)p.V, kSortBytes / row);
+    a.zero1 = std::max(a.zero0, p.V - kJoinBytes / row);
+  }
+  const int which = sort(p, s, Zeros{out, p.V, p.d, 0, MODE == SUM_DENSE ? a.zero0 : 0, out_dt}, st);
   a.dY = p.dY; a.order = s.buf[which]; a.segs = s.segs; a.valid = s.valid; a.parts = s.parts;
   a.V = p.V; a.T = p.T; a.d = p.d; a.scale = p.scale;
   a.groups = (int)((p.d + 32 * vec - 1) / (32 * vec));
@@ -394,8 +621,7 @@ int run_sums(const TokProblem& p, const TokScratch& s, int which, void* out, int
   a.out = out; a.out_dt = out_dt;
   if (r) { a.sq = r->sq; a.count = r->count; a.out_cap = r->cap; }
   a.sum_blocks = sum_blocks(p.T, p.d, vec);
-  const unsigned zeros = MODE == SUM_DENSE ? (unsigned)((p.V + 255) / 256) : 0u;
-  const dim3 grid(a.sum_blocks + zeros, p.K), join(a.sum_blocks, p.K);
+  const dim3 grid(a.sum_blocks + (unsigned)((a.zero1 - a.zero0 + 255) / 256), p.K), join(a.sum_blocks + (unsigned)((a.zero2 - a.zero1 + 255) / 256), p.K);
   if (p.y_dt == LORDO_F32) {
     if (vec == 4) launch_dep(window_sums_kernel<LORDO_F32, 4, MODE, kWindow>, grid, 256, 0, st, a);
     else launch_dep(window_sums_kernel<LORDO_F32, 1, MODE, kWindow>, grid, 256, 0, st, a);
@@ -406,7 +632,7 @@ int run_sums(const TokProblem& p, const TokScratch& s, int which, void* out, int
   if (vec == 8) launch_dep(join_sums_kernel<8, MODE, kWindow>, join, 256, 0, st, a);
   else if (vec == 4) launch_dep(join_sums_kernel<4, MODE, kWindow>, join, 256, 0, st, a);
   else launch_dep(join_sums_kernel<1, MODE, kWindow>, join, 256, 0, st, a);
-  return 2;
+  return 3;
 }
 
 }  // namespace
@@ -428,37 +654,14 @@ TokScratch tok_scratch(char* base, int K, long long V, long long d, long long ca
   return s;
 }
 
-int tok_sort(const TokProblem& p, const TokScratch& s, cudaStream_t st) {
-  const int bits = token_bits(p.V);
-  SortArgs a = {};
-  a.tokens = p.tokens; a.is64 = p.is64; a.K = p.K; a.T = p.T; a.cap = p.T; a.V = p.V;
-  a.passes = (bits + 7) / 8;
-  a.bits = (bits + a.passes - 1) / a.passes;
-  a.buf0 = s.buf[0]; a.buf1 = s.buf[1]; a.segs = s.segs; a.valid = s.valid;
-  int C = 1;
-  while (C < 8 && p.T > 2048ll * C) C *= 2;
-  const long long warps = (long long)C * kSortWarps;
-  a.per_warp = (int)(((p.T + warps - 1) / warps + 31) / 32 * 32);
-  cudaLaunchConfig_t lc = {};
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = C; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
-  lc.gridDim = dim3(C * p.K); lc.blockDim = dim3(kSortThreads); lc.stream = st;
-  lc.attrs = at; lc.numAttrs = 2;
-  cudaLaunchKernelEx(&lc, sort_tokens_kernel, a);
-  return (a.passes - 1) & 1;
-}
-
-int tok_dense(const TokProblem& p, const TokScratch& s, int which, void* dW, int w_dt, int accumulate, cudaStream_t st) {
-  return accumulate ? run_sums<SUM_ADD>(p, s, which, dW, w_dt, nullptr, st) : run_sums<SUM_DENSE>(p, s, which, dW, w_dt, nullptr, st);
+int tok_dense(const TokProblem& p, const TokScratch& s, void* dW, int w_dt, int accumulate, cudaStream_t st) {
+  return accumulate ? run_sums<SUM_ADD>(p, s, dW, w_dt, nullptr, st) : run_sums<SUM_DENSE>(p, s, dW, w_dt, nullptr, st);
 }
 
 long long tok_row_blocks_max(long long cap, long long d) { return 2ll * sum_blocks(cap, d, 1); }
 
-int tok_rows(const TokProblem& p, const TokScratch& s, int which, const TokRows& r, cudaStream_t st) {
-  return run_sums<SUM_ROWS>(p, s, which, r.rows, LORDO_F32, &r, st);
+int tok_rows(const TokProblem& p, const TokScratch& s, const TokRows& r, cudaStream_t st) {
+  return run_sums<SUM_ROWS>(p, s, r.rows, LORDO_F32, &r, st);
 }
 
 }  // namespace lordo
@@ -498,12 +701,14 @@ int lordo_embedding(const void* W, int w_dtype, int K, int64_t V, int64_t d, con
   if (cudaPeekAtLastError() != cudaSuccess) return LORDO_ERR_CUDA;
   const int full = w_dtype == LORDO_F32 ? 4 : 8;
   const int vec = wide(W, d, w_dtype) && (reinterpret_cast<uintptr_t>(out) & 15u) == 0 ? full : 1;
-  const long long pieces = (long long)K * T * ((d + vec - 1) / vec);
-  if ((pieces + 255) / 256 > 0x7fffffffll) return LORDO_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)((pieces + 255) / 256));
+  const long long rows = (long long)K * T, groups = (d + 32 * vec - 1) / (32 * vec);
+  const long long blocks = ((rows + kLookRows - 1) / kLookRows * groups + 7) / 8;
+  if (blocks > 0x7fffffffll) return LORDO_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)blocks);
   const int is64 = index == LORDO_I64;
-#define LORDO_LOOKUP(DT, VEC)                                                                                                                \
-  launch_dep(lookup_kernel<DT, VEC>, grid, 256, 0, st, W, tokens, is64, (long long)V, (long long)d, (long long)T, pieces, scale, out, out_dtype)
+#define LORDO_LOOKUP(DT, VEC)                                                                                                                  \
+  launch_dep(lookup_kernel<DT, VEC>, grid, 256, 0, st, W, tokens, is64, (long long)V, (long long)d, (long long)T, rows, (int)groups, scale, out, \
+             out_dtype)
   if (w_dtype == LORDO_F32) { if (vec > 1) LORDO_LOOKUP(LORDO_F32, 4); else LORDO_LOOKUP(LORDO_F32, 1); }
   else { if (vec > 1) LORDO_LOOKUP(LORDO_BF16, 8); else LORDO_LOOKUP(LORDO_BF16, 1); }
 #undef LORDO_LOOKUP
@@ -536,8 +741,7 @@ int lordo_embedding_grad(const void* dY, int y_dtype, const void* tokens, int in
   if ((size_t)s.bytes > workspace_bytes) return LORDO_ERR_NOMEM;
   if (cudaPeekAtLastError() != cudaSuccess) return LORDO_ERR_CUDA;
   TokProblem p = {tokens, index == LORDO_I64, K, V, T, d, dY, y_dtype, scale};
-  const int which = tok_sort(p, s, st);
-  tok_dense(p, s, which, dW, w_dtype, accumulate, st);
+  tok_dense(p, s, dW, w_dtype, accumulate, st);
   return cudaPeekAtLastError() == cudaSuccess ? LORDO_OK : LORDO_ERR_CUDA;
 }
 

@@ -27,11 +27,9 @@ struct TokProblem {
   float scale;
 };
 
-// Sorts every worker's tokens, ties by position; returns the buffer (0 or 1) that holds the order.
-int tok_sort(const TokProblem& p, const TokScratch& s, cudaStream_t st);
-// After tok_sort: dW[k][v] (in w_dt) = the sums, or += for the tokens that occur. Returns the launches.
-int tok_dense(const TokProblem& p, const TokScratch& s, int which, void* dW, int w_dt, int accumulate, cudaStream_t st);
-// After tok_sort: rows[k][i] (fp32, [K][cap][d]) = the sum of the token whose first sorted entry is i; sq[k][0 .. *count) = sums of their
+// Sorts every worker's tokens, ties by position, then dW[k][v] (in w_dt) = the sums, or += for the tokens that occur. Returns the launches.
+int tok_dense(const TokProblem& p, const TokScratch& s, void* dW, int w_dt, int accumulate, cudaStream_t st);
+// The same into rows[k][i] (fp32, [K][cap][d]) = the sum of the token whose first sorted entry is i; sq[k][0 .. *count) = sums of their
 // squares, *count at most tok_row_blocks_max.
 struct TokRows {
   float* rows;
@@ -40,7 +38,7 @@ struct TokRows {
   long long cap;
 };
 long long tok_row_blocks_max(long long cap, long long d);
-int tok_rows(const TokProblem& p, const TokScratch& s, int which, const TokRows& r, cudaStream_t st);
+int tok_rows(const TokProblem& p, const TokScratch& s, const TokRows& r, cudaStream_t st);
 
 // Argument checks: lordo_status. Limits are what the kernels' grids and 32-bit positions take.
 int check_tokens(int K, int64_t V, int64_t d, int64_t T, int index);

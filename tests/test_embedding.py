@@ -84,7 +84,7 @@ def test_binding_refuses_host_tensors(lib):
 # GPU
 # ---------------------------------------------------------------------------------------------
 SHAPES = [(1, 1, 1, 1), (1, 5, 8, 1), (2, 7, 3, 33), (3, 1000, 72, 257), (1, 50000, 16, 1000), (2, 255, 264, 4100), (2, 256, 40, 2049), (1, 70000, 8, 9001),
-          (1, 40, 1000, 63), (8, 300, 768, 96)]
+          (1, 40, 1000, 63), (8, 300, 768, 96), (2, 3000, 8, 20000), (2, 70000, 16, 30001)]
 
 
 @pytest.mark.gpu
