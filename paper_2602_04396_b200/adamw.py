@@ -20,6 +20,7 @@ from .lordo import LordoError, _AdamWBuffers, _AdamWConfig, _Grad, _Tensor, _dty
 
 _INDEX = {torch.int32: 0, torch.int64: 1}
 _STATES = {"f32": 0, "8bit": 1}
+_raw_stream = torch._C._cuda_getCurrentRawStream  # without the object that torch.cuda.current_stream builds
 BLOCK = 256  # elements per scale of the 8-bit moments
 
 
@@ -127,7 +128,7 @@ class AdamW:
             raise LordoError(rc, where, self.lib.lordo_adamw_last_error(self._ctx).decode())
 
     def _stream(self, stream: Optional[torch.cuda.Stream]) -> int:
-        return (stream if stream is not None else torch.cuda.current_stream(self.device)).cuda_stream
+        return stream.cuda_stream if stream is not None else _raw_stream(self.device.index)
 
     def _token_grad(self, i: int, g: TokenGrad) -> int:
         """Fills the gradient's entry but for the address of dY, which is returned."""

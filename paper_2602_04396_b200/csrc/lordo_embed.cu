@@ -112,10 +112,13 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(SortArgs a) {
     cluster_sync_all();
     int all = 0, before = 0;
     if (t < R) {
-      for (unsigned r = 0; r < C; ++r) {
-        const int n = cluster_load(tot + t, r);
-        all += n;
-        if (r < c) before += n;
+      int n[8];
+#pragma unroll
+      for (unsigned r = 0; r < 8; ++r) n[r] = r < C ? cluster_load(tot + t, r) : 0;
+#pragma unroll
+      for (unsigned r = 0; r < 8; ++r) {
+        all += n[r];
+        if (r < c) before += n[r];
       }
     }
     int scan = all;
@@ -215,23 +218,36 @@ __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(SortArgs a) {
       __syncwarp();
     }
     __syncthreads();
-    for (int x = w; x < R; x += kSortWarps) {
-      const int n = cnt[x][lane];
-      int scan = n;
+    // a warp scans eight digits at a time, side by side
+    for (int x0 = 8 * w; x0 < R; x0 += 8 * kSortWarps) {
+      int n[8], sum[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) sum[x] = n[x] = x0 + x < R ? cnt[x0 + x][lane] : 0;
+#pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const int up = __shfl_up_sync(0xffffffffu, scan, o);
-        if (lane >= o) scan += up;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const int up = __shfl_up_sync(0xffffffffu, sum[x], o);
+          if (lane >= o) sum[x] += up;
+        }
       }
-      cnt[x][lane] = (unsigned short)(scan - n);
-      if (lane == 31) tot[x] = scan;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        if (x0 + x >= R) break;
+        cnt[x0 + x][lane] = (unsigned short)(sum[x] - n[x]);
+        if (lane == 31) tot[x0 + x] = sum[x];
+      }
     }
     if (C > 1) cluster_sync_all(); else __syncthreads();
     int all = 0, before = 0;
     if (t < R) {
-      for (unsigned r = 0; r < C; ++r) {
-        const int n = cluster_load(tot + t, r);
-        all += n;
-        if (r < c) before += n;
+      int n[8];
+#pragma unroll
+      for (unsigned r = 0; r < 8; ++r) n[r] = r < C ? cluster_load(tot + t, r) : 0;
+#pragma unroll
+      for (unsigned r = 0; r < 8; ++r) {
+        all += n[r];
+        if (r < c) before += n[r];
       }
     }
     int scan = all;
@@ -266,7 +282,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(SortArgs a) {
       if (begin + 32 * b < T) e[b] = buf[w * (32 * NB) + lane + 32 * b];
   }
   auto token_at = [&](int i) {  // of the order, in whichever CTA's shared memory
-    return i < 0 || i >= T ? -1 : cluster_load(&buf[i % L].x, (unsigned)(i / L));
+    return i < 0 || i >= T ? -1 : i / L == (int)c ? buf[i % L].x : cluster_load(&buf[i % L].x, (unsigned)(i / L));
   };
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
@@ -338,15 +354,37 @@ struct SumArgs {
   void* out;
   int out_dt;
   double* sq;           // [K][2 * gridDim.x]
-  int* count;           // 2 * gridDim.x
+  int* count;           // of sums of squares: 2 * gridDim.x, or gridDim.x where nothing is joined
   long long out_cap;    // rows of a worker in `out` (sums in rows of their own)
   unsigned sum_blocks;  // blocks that form sums; the rest write the zeros of rows without a token,
   long long zero0, zero1, zero2;  // [zero0, zero1) beside the windows, [zero1, zero2) beside the joining
 };
 
-// The sum of token v, whose first sorted entry is `start`.
-template <int VEC, int MODE>
-__device__ __forceinline__ void emit(const SumArgs& a, int k, int v, int start, long long col, float (&acc)[VEC], float& sq) {
+// What a row of the table holds before it is added to.
+template <int ODT, int VEC>
+struct Old {
+  unsigned r[ODT == LORDO_F32 ? VEC : (VEC + 1) / 2];
+  __device__ __forceinline__ void load(const void* base, long long at) {
+    if constexpr (VEC == 1) {
+      r[0] = ODT == LORDO_F32 ? reinterpret_cast<const unsigned*>(base)[at] : reinterpret_cast<const unsigned short*>(base)[at];
+    } else {
+      constexpr int kWords = ODT == LORDO_F32 ? VEC : VEC / 2;
+      const char* p = reinterpret_cast<const char*>(base) + at * (ODT == LORDO_F32 ? 4 : 2);
+#pragma unroll
+      for (int j = 0; j < kWords; j += 2) {
+        const uint2 x = reinterpret_cast<const uint2*>(p)[j / 2];
+        r[j] = x.x; r[j + 1] = x.y;
+      }
+    }
+  }
+  __device__ __forceinline__ float value(int j) const {
+    return ODT == LORDO_F32 ? __uint_as_float(r[j]) : __uint_as_float(j & 1 ? r[j / 2] & 0xFFFF0000u : r[j / 2] << 16);
+  }
+};
+
+// The sum of token v, whose first sorted entry is `start`; old: the row it is added to.
+template <int VEC, int MODE, int ODT>
+__device__ __forceinline__ void emit(const SumArgs& a, int k, int v, int start, long long col, float (&acc)[VEC], const Old<ODT, VEC>& old, float& sq) {
 #pragma unroll
   for (int j = 0; j < VEC; ++j) acc[j] *= a.scale;
   if (MODE == SUM_ROWS) {
@@ -354,12 +392,11 @@ __device__ __forceinline__ void emit(const SumArgs& a, int k, int v, int start, 
 #pragma unroll
     for (int j = 0; j < VEC; ++j) sq += acc[j] * acc[j];
   } else {
-    const long long at = ((long long)k * a.V + v) * a.d + col;
     if (MODE == SUM_ADD) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) acc[j] += load1(a.out, a.out_dt, at + j);
+      for (int j = 0; j < VEC; ++j) acc[j] += old.value(j);
     }
-    put<VEC>(a.out, a.out_dt, at, acc);
+    put<VEC>(a.out, ODT, ((long long)k * a.V + v) * a.d + col, acc);
   }
 }
 
@@ -373,15 +410,15 @@ __device__ __forceinline__ void block_squares(const SumArgs& a, int k, int which
   if (threadIdx.x == 0) {
     s = 0.0;
     for (int w = 0; w < 8; ++w) s += red[w];
-    a.sq[(long long)k * 2 * gridDim.x + which * gridDim.x + blockIdx.x] = s;
-    if (k == 0 && blockIdx.x == 0) *a.count = 2 * (int)gridDim.x;
+    a.sq[((long long)k * (a.windows > 1 ? 2 : 1) + which) * gridDim.x + blockIdx.x] = s;
+    if (k == 0 && blockIdx.x == 0) *a.count = (a.windows > 1 ? 2 : 1) * (int)gridDim.x;
   }
 }
 
 // A warp walks a window of W sorted entries, 32 * VEC columns of each row of dY, eight rows under way at a time. Tokens whose entries all lie in
 // the window are done; the first part of one that goes on and the last of one that came in are left for join_sums_kernel.
 constexpr int kAhead = 8;
-template <int DT, int VEC, int MODE, int W>
+template <int DT, int VEC, int MODE, int W, int ODT>
 __device__ __forceinline__ void window_sums(const SumArgs& a, int k, int w, long long col, int lane, float& sq) {
   const int valid = a.valid[k], s = w * W;
   if (s >= valid) return;
@@ -400,10 +437,15 @@ __device__ __forceinline__ void window_sums(const SumArgs& a, int k, int w, long
   const long long first = (long long)k * a.T * a.d + (on ? col : 0);
   for (int b = 0; b < n; b += kAhead) {
     Piece<DT, VEC> x[kAhead];
+    Old<ODT, VEC> old[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const int pos = __shfl_sync(0xffffffffu, mine.y, (b + j) & 31);
       if (b + j < n && on) x[j].load(a.dY, first + (long long)pos * a.d);
+      if (MODE == SUM_ADD) {
+        const int v = __shfl_sync(0xffffffffu, mine.x, (b + j) & 31);
+        if (on && ((ends >> ((b + j) & 31)) & 1u)) old[j].load(a.out, ((long long)k * a.V + v) * a.d + col);
+      }
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
@@ -416,7 +458,7 @@ __device__ __forceinline__ void window_sums(const SumArgs& a, int k, int w, long
 #pragma unroll
             for (int i = 0; i < VEC; ++i) part[i] = acc[i];
           } else {
-            emit<VEC, MODE>(a, k, v, start, col, acc, sq);
+            emit<VEC, MODE, ODT>(a, k, v, start, col, acc, old[j], sq);
           }
         }
 #pragma unroll
@@ -446,7 +488,7 @@ __device__ __forceinline__ void empty_rows(const SumArgs& a, int k, long long v0
   }
 }
 
-template <int DT, int VEC, int MODE, int W>
+template <int DT, int VEC, int MODE, int W, int ODT>
 __global__ void __launch_bounds__(256) window_sums_kernel(SumArgs a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = blockIdx.y;
   dep_begin();
@@ -457,12 +499,12 @@ __global__ void __launch_bounds__(256) window_sums_kernel(SumArgs a) {
   const long long item = (long long)blockIdx.x * 8 + warp;
   const long long w = item / a.groups;
   float sq = 0.f;
-  if (w < a.windows) window_sums<DT, VEC, MODE, W>(a, k, (int)w, ((item - w * a.groups) * 32 + lane) * VEC, lane, sq);
+  if (w < a.windows) window_sums<DT, VEC, MODE, W, ODT>(a, k, (int)w, ((item - w * a.groups) * 32 + lane) * VEC, lane, sq);
   if (MODE == SUM_ROWS) block_squares(a, k, 0, sq);
 }
 
 // Tokens whose entries begin in one window and go on in others: their parts in the order of the windows.
-template <int VEC, int MODE, int W>
+template <int VEC, int MODE, int W, int ODT>
 __global__ void __launch_bounds__(256) join_sums_kernel(SumArgs a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = blockIdx.y;
   dep_begin();
@@ -483,6 +525,8 @@ __global__ void __launch_bounds__(256) join_sums_kernel(SumArgs a) {
       if (seg.x >= w * W && col < a.d) {  // it begins here
         const float* p = a.parts + ((long long)k * a.windows + w) * 2 * a.d + a.d + col;
         float acc[VEC];
+        Old<ODT, VEC> old;
+        if (MODE == SUM_ADD) old.load(a.out, ((long long)k * a.V + v) * a.d + col);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) acc[i] = __ldcg(p + i);
         const int end = (seg.y - 1) / W;
@@ -499,7 +543,7 @@ __global__ void __launch_bounds__(256) join_sums_kernel(SumArgs a) {
 #pragma unroll
             for (int i = 0; i < VEC; ++i) acc[i] += y[j][i];
         }
-        emit<VEC, MODE>(a, k, v, seg.x, col, acc, sq);
+        emit<VEC, MODE, ODT>(a, k, v, seg.x, col, acc, old, sq);
       }
     }
   }
@@ -572,7 +616,7 @@ unsigned sum_blocks(long long T, long long d, int vec) {
 // Which rows' zeros are written when. While tokens are sorted the memory is idle, so a first part of the table is zeroed then without
 // knowing which rows will have a token; as much more as the joining takes is left to it. What is left is written beside the windows. (All of it
 // there: 50304 x 768, K = 8, 16384 tokens 188 us.)
-constexpr long long kSortBytes = 64ll << 20, kJoinBytes = 64ll << 20;
+constexpr long long kSortBytes = 64ll << 20, kJoinBytes = 128ll << 20;
 
 int sort(const TokProblem& p, const TokScratch& s, const Zeros& zeros, cudaStream_t st) {
   const int bits = token_bits(p.V);
@@ -587,7 +631,7 @@ int sort(const TokProblem& p, const TokScratch& s, const Zeros& zeros, cudaStrea
   const long long warps = (long long)C * kSortWarps;
   a.per_warp = (int)(((p.T + warps - 1) / warps + 31) / 32 * 32);
   a.clusters = (unsigned)p.K;
-  const unsigned fill = zeros.last > zeros.first ? (unsigned)((128 + C - 1) / C * C) : 0u;
+  const unsigned fill = zeros.last > zeros.first ? (unsigned)((80 + C - 1) / C * C) : 0u;
   cudaLaunchConfig_t lc = {};
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -622,17 +666,20 @@ int run_sums(const TokProblem& p, const TokScratch& s, void* out, int out_dt, co
   if (r) { a.sq = r->sq; a.count = r->count; a.out_cap = r->cap; }
   a.sum_blocks = sum_blocks(p.T, p.d, vec);
   const dim3 grid(a.sum_blocks + (unsigned)((a.zero1 - a.zero0 + 255) / 256), p.K), join(a.sum_blocks + (unsigned)((a.zero2 - a.zero1 + 255) / 256), p.K);
-  if (p.y_dt == LORDO_F32) {
-    if (vec == 4) launch_dep(window_sums_kernel<LORDO_F32, 4, MODE, kWindow>, grid, 256, 0, st, a);
-    else launch_dep(window_sums_kernel<LORDO_F32, 1, MODE, kWindow>, grid, 256, 0, st, a);
-  } else {
-    if (vec == 8) launch_dep(window_sums_kernel<LORDO_BF16, 8, MODE, kWindow>, grid, 256, 0, st, a);
-    else launch_dep(window_sums_kernel<LORDO_BF16, 1, MODE, kWindow>, grid, 256, 0, st, a);
+  const bool joins = a.windows > 1 || a.zero2 > a.zero1;  // else no token lies in two windows
+#define LORDO_SUMS(DT, VEC, ODT)                                                              \
+  launch_dep(window_sums_kernel<DT, VEC, MODE, kWindow, ODT>, grid, 256, 0, st, a);           \
+  if (joins) launch_dep(join_sums_kernel<VEC, MODE, kWindow, ODT>, join, 256, 0, st, a)
+#define LORDO_SUMS_VEC(DT, FULL, ODT) \
+  if (vec > 1) { LORDO_SUMS(DT, FULL, ODT); } else { LORDO_SUMS(DT, 1, ODT); }
+  if (out_dt == LORDO_F32) {
+    if (p.y_dt == LORDO_F32) { LORDO_SUMS_VEC(LORDO_F32, 4, LORDO_F32) } else { LORDO_SUMS_VEC(LORDO_BF16, 8, LORDO_F32) }
+  } else if constexpr (MODE != SUM_ROWS) {
+    if (p.y_dt == LORDO_F32) { LORDO_SUMS_VEC(LORDO_F32, 4, LORDO_BF16) } else { LORDO_SUMS_VEC(LORDO_BF16, 8, LORDO_BF16) }
   }
-  if (vec == 8) launch_dep(join_sums_kernel<8, MODE, kWindow>, join, 256, 0, st, a);
-  else if (vec == 4) launch_dep(join_sums_kernel<4, MODE, kWindow>, join, 256, 0, st, a);
-  else launch_dep(join_sums_kernel<1, MODE, kWindow>, join, 256, 0, st, a);
-  return 3;
+#undef LORDO_SUMS_VEC
+#undef LORDO_SUMS
+  return joins ? 3 : 2;
 }
 
 }  // namespace
