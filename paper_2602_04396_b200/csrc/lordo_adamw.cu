@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(256) adamw_norm_kernel(const __grid_constant__
       const float x = load1(G, GDT, edge);
       s += (double)x * (double)x;
     }
-  } else if (q == tab.start[i]) {  // its first chunk stands for the whole tensor
+  } else {  // one chunk stands for the whole tensor
     const int count = *T.rowsq_count;
     const double* p = T.rowsq + (long long)k * count;
     for (int x = t; x < count; x += 256) s += __ldcg(p + x);
@@ -617,115 +617,150 @@ __global__ void __launch_bounds__(256, 4) adamw_step8_kernel(const __grid_consta
 // X0 <- X0 - eta (D + mu B); every W_k <- X0. Each operation is rounded on its own: with bf16 weights D of the next synchronisation is
 // what X0 loses in its cast, and a last bit that depends on what a compiler fuses would become a whole step of bf16 there.
 // ---------------------------------------------------------------------------------------------
+// The three arrays of a tensor (weights, first, second moments) are blocks of their own, blockIdx.y, of 2048 elements of all workers. What counts is
+// how many loads an SM has under way: 50304 x 768, K = 8, fp32 moments 1032 us with eight blocks an SM (32 registers), 1064 with six, 1074 with
+// four, 1117 with one block of 4096 for all three arrays; 8-bit moments 610, with eight blocks (spilling) 645, with four 657.
+constexpr int kOuterItems = 2;  // per thread, at a distance of a block's threads: all their loads of a worker are under way together
+
 template <int WDT, int N>  // N consecutive elements of every worker: 4 (a float4's alignment everywhere) or 1
-__device__ __forceinline__ void outer_weights(const AwTensor& T, int K, const AwOuter& o, float inv_k, long long e) {
-  float s[N] = {}, x0[N], b[N];
-#pragma unroll 4
+__device__ __forceinline__ void outer_weights(const AwTensor& T, int K, const AwOuter& o, float inv_k, long long e0, long long e1) {
+  float s[kOuterItems][N] = {};
   for (int k = 0; k < K; ++k) {
-    if constexpr (N == 4) {
-      const float4 w = load4(T.W, WDT, (long long)k * T.n + e);
-      s[0] += w.x; s[1] += w.y; s[2] += w.z; s[3] += w.w;
-    } else {
-      s[0] += load1(T.W, WDT, (long long)k * T.n + e);
+#pragma unroll
+    for (int x = 0; x < kOuterItems; ++x) {
+      const long long e = e0 + x * 256 * N;
+      if (e >= e1) break;
+      if constexpr (N == 4) {
+        const float4 w = load4(T.W, WDT, (long long)k * T.n + e);
+        s[x][0] += w.x; s[x][1] += w.y; s[x][2] += w.z; s[x][3] += w.w;
+      } else {
+        s[x][0] += load1(T.W, WDT, (long long)k * T.n + e);
+      }
     }
   }
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    x0[j] = T.X0[e + j];
-    const float d = __fsub_rn(x0[j], __fmul_rn(s[j], inv_k));
-    if (o.nesterov) {
-      b[j] = __fadd_rn(__fmul_rn(o.mu, T.B[e + j]), d);
-      x0[j] = __fsub_rn(x0[j], __fmul_rn(o.eta, __fadd_rn(d, __fmul_rn(o.mu, b[j]))));
-    } else {
-      x0[j] -= d;
+  for (int x = 0; x < kOuterItems; ++x) {
+    const long long e = e0 + x * 256 * N;
+    if (e >= e1) break;
+    float x0[N], b[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      x0[j] = T.X0[e + j];
+      const float d = __fsub_rn(x0[j], __fmul_rn(s[x][j], inv_k));
+      if (o.nesterov) {
+        b[j] = __fadd_rn(__fmul_rn(o.mu, T.B[e + j]), d);
+        x0[j] = __fsub_rn(x0[j], __fmul_rn(o.eta, __fadd_rn(d, __fmul_rn(o.mu, b[j]))));
+      } else {
+        x0[j] -= d;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      T.X0[e + j] = x0[j];
+      if (o.nesterov) T.B[e + j] = b[j];
+      s[x][j] = x0[j];
     }
   }
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    T.X0[e + j] = x0[j];
-    if (o.nesterov) T.B[e + j] = b[j];
-  }
-#pragma unroll 4
   for (int k = 0; k < K; ++k) {
-    if constexpr (N == 4) store4(T.W, WDT, (long long)k * T.n + e, make_float4(x0[0], x0[1], x0[2], x0[3]));
-    else store1(T.W, WDT, (long long)k * T.n + e, x0[0]);
+#pragma unroll
+    for (int x = 0; x < kOuterItems; ++x) {
+      const long long e = e0 + x * 256 * N;
+      if (e >= e1) break;
+      if constexpr (N == 4) store4(T.W, WDT, (long long)k * T.n + e, make_float4(s[x][0], s[x][1 % N], s[x][2 % N], s[x][3 % N]));
+      else store1(T.W, WDT, (long long)k * T.n + e, s[x][0]);
+    }
   }
 }
 
 template <int N>
-__device__ __forceinline__ void outer_mean(float* p, long long n, int K, float inv_k, long long e) {
-  float s[N] = {};
-#pragma unroll 4
+__device__ __forceinline__ void outer_mean(float* p, long long n, int K, float inv_k, long long e0, long long e1) {
+  float s[kOuterItems][N] = {};
   for (int k = 0; k < K; ++k) {
-    if constexpr (N == 4) {
-      const float4 x = *reinterpret_cast<const float4*>(p + (long long)k * n + e);
-      s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
-    } else {
-      s[0] += p[(long long)k * n + e];
-    }
-  }
 #pragma unroll
-  for (int j = 0; j < N; ++j) s[j] *= inv_k;
-#pragma unroll 4
-  for (int k = 0; k < K; ++k) {
-    if constexpr (N == 4) *reinterpret_cast<float4*>(p + (long long)k * n + e) = make_float4(s[0], s[1], s[2], s[3]);
-    else p[(long long)k * n + e] = s[0];
-  }
-}
-
-template <int WDT>
-__global__ void __launch_bounds__(256) adamw_outer_kernel(AwLaunch l, const unsigned* __restrict__ start, AwOuter o) {
-  const int i = find_tensor(start, l.count, blockIdx.x);
-  const AwTensor T = l.tensors[i];
-  dep_begin();
-  const float inv_k = 1.f / (float)l.K;
-  const long long e0 = (long long)(blockIdx.x - start[i]) * kAwOuter;
-  const long long e1 = e0 + kAwOuter < T.n ? e0 + kAwOuter : T.n;
-  if (T.n % 4 == 0) {
-    for (long long e = e0 + 4 * threadIdx.x; e < e1; e += 1024) {
-      outer_weights<WDT, 4>(T, l.K, o, inv_k, e);
-      if (o.sync_m) outer_mean<4>(reinterpret_cast<float*>(T.m), T.n, l.K, inv_k, e);
-      if (o.sync_v) outer_mean<4>(reinterpret_cast<float*>(T.v), T.n, l.K, inv_k, e);
-    }
-  } else {
-    for (long long e = e0 + threadIdx.x; e < e1; e += 256) {
-      outer_weights<WDT, 1>(T, l.K, o, inv_k, e);
-      if (o.sync_m) outer_mean<1>(reinterpret_cast<float*>(T.m), T.n, l.K, inv_k, e);
-      if (o.sync_v) outer_mean<1>(reinterpret_cast<float*>(T.v), T.n, l.K, inv_k, e);
-    }
-  }
-}
-
-// Mean over the workers of one array of 8-bit moments, one block of 256 of every worker: a lane has eight elements.
-template <bool SECOND>
-__device__ __forceinline__ void outer_mean8(const AwTensor& T, int K, float inv_k, unsigned long long key, long long b, long long e, int left, int lane) {
-  unsigned char* C = reinterpret_cast<unsigned char*>(SECOND ? T.v : T.m);
-  unsigned char* S = SECOND ? T.vs : T.ms;
-  const bool vec = left == 8 && (T.n & 7) == 0;
-  float2 a[4] = {};
-  for (int k = 0; k < K; ++k) {
-    const float scale = pow2(S[(long long)k * T.nb + b]);
-    const unsigned char* p = C + (long long)k * T.n + e;
-    unsigned c[2] = {0u, 0u};
-    if (vec) {
-      const uint2 x = *reinterpret_cast<const uint2*>(p);
-      c[0] = x.x; c[1] = x.y;
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < left) c[j >> 2] |= (unsigned)p[j] << (8 * (j & 3));
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float2 x[2];
-      values8(c[h], x);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float2 y = __fmul2_rn(x[j], both(scale));
-        a[2 * h + j] = SECOND ? __ffma2_rn(y, y, a[2 * h + j]) : __fadd2_rn(a[2 * h + j], y);
+    for (int x = 0; x < kOuterItems; ++x) {
+      const long long e = e0 + x * 256 * N;
+      if (e >= e1) break;
+      if constexpr (N == 4) {
+        const float4 v = *reinterpret_cast<const float4*>(p + (long long)k * n + e);
+        s[x][0] += v.x; s[x][1] += v.y; s[x][2] += v.z; s[x][3] += v.w;
+      } else {
+        s[x][0] += p[(long long)k * n + e];
       }
     }
   }
+#pragma unroll
+  for (int x = 0; x < kOuterItems; ++x)
+#pragma unroll
+    for (int j = 0; j < N; ++j) s[x][j] *= inv_k;
+  for (int k = 0; k < K; ++k) {
+#pragma unroll
+    for (int x = 0; x < kOuterItems; ++x) {
+      const long long e = e0 + x * 256 * N;
+      if (e >= e1) break;
+      if constexpr (N == 4) *reinterpret_cast<float4*>(p + (long long)k * n + e) = make_float4(s[x][0], s[x][1 % N], s[x][2 % N], s[x][3 % N]);
+      else p[(long long)k * n + e] = s[x][0];
+    }
+  }
+}
+
+// Eight codes of a lane, at p; WHOLE: of a whole block at an address that is a multiple of 8, else `left` of them.
+template <bool WHOLE>
+__device__ __forceinline__ uint2 load_codes(const unsigned char* p, int left) {
+  if constexpr (WHOLE) {
+    return *reinterpret_cast<const uint2*>(p);
+  } else {
+    unsigned c[2] = {0u, 0u};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < left) c[j >> 2] |= (unsigned)p[j] << (8 * (j & 3));
+    return make_uint2(c[0], c[1]);
+  }
+}
+template <bool WHOLE>
+__device__ __forceinline__ void store_codes(unsigned char* p, int left, const unsigned (&c)[2]) {
+  if constexpr (WHOLE) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(c[0], c[1]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < left) p[j] = (unsigned char)(c[j >> 2] >> (8 * (j & 3)));
+  }
+}
+
+// Mean over the workers of a block of 256 of 8-bit moments: a lane has eight elements; four workers' codes are under way together.
+template <bool SECOND, bool WHOLE>
+__device__ __forceinline__ void outer_mean8(const AwTensor& T, int K, float inv_k, unsigned long long key, long long b, int lane) {
+  const long long e = b * kAwBlock + 8 * lane;
+  unsigned char* C = reinterpret_cast<unsigned char*>(SECOND ? T.v : T.m) + e;
+  unsigned char* S = (SECOND ? T.vs : T.ms) + b;
+  const int left = e >= T.n ? 0 : T.n - e < 8 ? (int)(T.n - e) : 8;
+  float2 a[4] = {};
+  auto add = [&](uint2 c, int scale) {
+    const float2 s = both(pow2(scale));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float2 z[2];
+      values8(h ? c.y : c.x, z);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float2 y = __fmul2_rn(z[j], s);
+        a[2 * h + j] = SECOND ? __ffma2_rn(y, y, a[2 * h + j]) : __fadd2_rn(a[2 * h + j], y);
+      }
+    }
+  };
+  int k = 0;
+  for (; k + 4 <= K; k += 4) {
+    uint2 c[4];
+    int scale[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      c[x] = load_codes<WHOLE>(C + (long long)(k + x) * T.n, left);
+      scale[x] = S[(long long)(k + x) * T.nb];
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) add(c[x], scale[x]);
+  }
+  for (; k < K; ++k) add(load_codes<WHOLE>(C + (long long)k * T.n, left), S[(long long)k * T.nb]);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     a[j] = __fmul2_rn(a[j], both(inv_k));
@@ -741,51 +776,49 @@ __device__ __forceinline__ void outer_mean8(const AwTensor& T, int K, float inv_
     const float2 x[2] = {a[2 * h], a[2 * h + 1]};
     c[h] = pack8<PACK_ANY, SECOND>(x, inv, u);
   }
-  for (int k = 0; k < K; ++k) {
-    unsigned char* p = C + (long long)k * T.n + e;
-    if (vec) {
-      *reinterpret_cast<uint2*>(p) = make_uint2(c[0], c[1]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < left) p[j] = (unsigned char)(c[j >> 2] >> (8 * (j & 3)));
-    }
-  }
+  for (k = 0; k < K; ++k) store_codes<WHOLE>(C + (long long)k * T.n, left, c);
   __syncwarp();  // every lane has read the scales
-  for (int k = lane; k < K; k += 32) S[(long long)k * T.nb + b] = (unsigned char)code;
+  for (k = lane; k < K; k += 32) S[(long long)k * T.nb] = (unsigned char)code;
 }
 
-template <int WDT>
-__global__ void __launch_bounds__(256) adamw_outer8_kernel(AwLaunch l, const unsigned* __restrict__ start, AwOuter o) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+template <int WDT, bool SMALL>
+__global__ void __launch_bounds__(256, SMALL ? 6 : 8) adamw_outer_kernel(AwLaunch l, const unsigned* __restrict__ start, AwOuter o) {
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5, array = blockIdx.y;
   const int i = find_tensor(start, l.count, blockIdx.x);
   const AwTensor T = l.tensors[i];
   const unsigned long long key = mix64(o.key + kGolden * ((unsigned long long)T.index + 1));
   dep_begin();
+  if ((array == 1 && !o.sync_m) || (array == 2 && !o.sync_v)) return;
   const float inv_k = 1.f / (float)l.K;
-  const long long b0 = (long long)(blockIdx.x - start[i]) * (kAwOuter / kAwBlock);
-  for (int x = warp; x < kAwOuter / kAwBlock; x += 8) {
-    const long long b = b0 + x;
-    if (b >= T.nb) break;
-    const long long at = b * kAwBlock, e = at + 8 * lane;
-    const int left = e >= T.n ? 0 : T.n - e < 8 ? (int)(T.n - e) : 8;
-    if (T.n % 4 == 0) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (at + 128 * h + 4 * lane < T.n) outer_weights<WDT, 4>(T, l.K, o, inv_k, at + 128 * h + 4 * lane);
-    } else {
-      for (int j = lane; j < kAwBlock && at + j < T.n; j += 32) outer_weights<WDT, 1>(T, l.K, o, inv_k, at + j);
+  const long long e0 = (long long)(blockIdx.x - start[i]) * l.piece;
+  const long long e1 = e0 + l.piece < T.n ? e0 + l.piece : T.n;
+  const bool four = T.n % 4 == 0;
+  if (array && SMALL) {
+    for (long long b = e0 / kAwBlock + warp; b * kAwBlock < e1; b += 8) {
+      const bool whole = (T.n & 7) == 0 && (b + 1) * kAwBlock <= T.n;
+      if (array == 1) {
+        if (whole) outer_mean8<false, true>(T, l.K, inv_k, key, b, lane); else outer_mean8<false, false>(T, l.K, inv_k, key, b, lane);
+      } else {
+        if (whole) outer_mean8<true, true>(T, l.K, inv_k, key, b, lane); else outer_mean8<true, false>(T, l.K, inv_k, key, b, lane);
+      }
     }
-    if (o.sync_m) outer_mean8<false>(T, l.K, inv_k, key, b, e, left, lane);
-    if (o.sync_v) outer_mean8<true>(T, l.K, inv_k, key, b, e, left, lane);
+    return;
+  }
+  float* p = reinterpret_cast<float*>(array == 1 ? T.m : T.v);
+  for (long long e = e0 + (four ? 4 * t : t); e < e1; e += kOuterItems * 256 * (four ? 4 : 1)) {
+    if (four) {
+      if (array == 0) outer_weights<WDT, 4>(T, l.K, o, inv_k, e, e1); else outer_mean<4>(p, T.n, l.K, inv_k, e, e1);
+    } else {
+      if (array == 0) outer_weights<WDT, 1>(T, l.K, o, inv_k, e, e1); else outer_mean<1>(p, T.n, l.K, inv_k, e, e1);
+    }
   }
 }
 
 __global__ void __launch_bounds__(256) adamw_init_kernel(AwLaunch l, const unsigned* __restrict__ start) {
   const int i = find_tensor(start, l.count, blockIdx.x);
   const AwTensor T = l.tensors[i];
-  const long long e0 = (long long)(blockIdx.x - start[i]) * kAwOuter;
-  const long long e1 = e0 + kAwOuter < T.n ? e0 + kAwOuter : T.n;
+  const long long e0 = (long long)(blockIdx.x - start[i]) * l.piece;
+  const long long e1 = e0 + l.piece < T.n ? e0 + l.piece : T.n;
   for (long long e = e0 + threadIdx.x; e < e1; e += 256) {
     const float w = load1(T.W, l.w_dt, e);
     if (T.X0) T.X0[e] = w;
@@ -827,13 +860,13 @@ void launch_aw_step(const AwLaunch& l, const AwTable& t, const float* coef, int 
 }
 
 void launch_aw_outer(const AwLaunch& l, const unsigned* start, const AwOuter& o, cudaStream_t st) {
-  const dim3 grid(l.units);
+  const dim3 grid(l.units, 3);
   if (l.small) {
-    if (l.w_dt == LORDO_F32) launch_dep(adamw_outer8_kernel<LORDO_F32>, grid, 256, 0, st, l, start, o);
-    else launch_dep(adamw_outer8_kernel<LORDO_BF16>, grid, 256, 0, st, l, start, o);
+    if (l.w_dt == LORDO_F32) launch_dep(adamw_outer_kernel<LORDO_F32, true>, grid, 256, 0, st, l, start, o);
+    else launch_dep(adamw_outer_kernel<LORDO_BF16, true>, grid, 256, 0, st, l, start, o);
   } else {
-    if (l.w_dt == LORDO_F32) launch_dep(adamw_outer_kernel<LORDO_F32>, grid, 256, 0, st, l, start, o);
-    else launch_dep(adamw_outer_kernel<LORDO_BF16>, grid, 256, 0, st, l, start, o);
+    if (l.w_dt == LORDO_F32) launch_dep(adamw_outer_kernel<LORDO_F32, false>, grid, 256, 0, st, l, start, o);
+    else launch_dep(adamw_outer_kernel<LORDO_BF16, false>, grid, 256, 0, st, l, start, o);
   }
 }
 

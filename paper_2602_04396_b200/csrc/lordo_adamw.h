@@ -1,5 +1,7 @@
 // Internal interface between the host layer of the AdamW groups (lordo_adamw_api.cu) and their kernels (lordo_adamw.cu).
 #pragma once
+#include <algorithm>
+
 #include "lordo_common.cuh"
 
 namespace lordo {
@@ -10,7 +12,7 @@ inline long long aw_piece(long long elements) {
   const long long p = (elements / (148 * 8) + 2047) / 2048 * 2048;
   return p < 2048 ? 2048 : p > 32768 ? 32768 : p;
 }
-constexpr int kAwOuter = 4096;   // elements of a tensor that a CTA of the synchronisation works on
+constexpr int kAwOuter = 2048;   // elements of one worker's tensor that a CTA of the synchronisation works on, for all workers
 constexpr int kAwTable = 512;    // tensors of one launch
 
 // One tensor, built once and kept in the workspace. Arrays are [K][n]; X0, B are [n].
@@ -52,7 +54,7 @@ struct AwLaunch {
   int count, K;
   unsigned units;           // per worker
   int w_dt, g_dt, small;    // small: 8-bit moments
-  int piece;                // elements behind a unit of the step
+  int piece;                // elements behind a unit
 };
 
 struct AwClip {

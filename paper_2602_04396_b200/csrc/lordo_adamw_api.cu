@@ -16,7 +16,7 @@ namespace {
 struct Group {
   int first = 0, count = 0;
   unsigned chunks = 0, chunks_before = 0, pieces = 0, blocks = 0;
-  AwTable norm, step;           // `start` is set once, `G` by every step
+  AwTable norm, step;           // `G`, and the chunks that the norm's `start` counts, are set by every step
   std::vector<unsigned> outer;  // first block of every tensor
   unsigned* d_outer = nullptr;
 };
@@ -42,7 +42,7 @@ struct lordo_adamw_ctx {
   unsigned *d_tickets = nullptr, *d_status = nullptr;
   float* d_coef = nullptr;
   size_t n_tickets = 0;
-  unsigned total_chunks = 0;
+  unsigned total_chunks = 0;  // most of a worker in one step
   int piece = 0, chunk = 0;
   int64_t steps = 0, outers = 0, launches = 0;
   std::string err;
@@ -112,18 +112,17 @@ size_t build(lordo_adamw_ctx* c, const lordo_adamw_buffers* buf, char* base) {
     Group& g = c->groups.back();
     g.first = first;
     g.count = nt - first < kAwTable ? nt - first : kAwTable;
-    g.chunks_before = c->total_chunks;
     for (int x = 0; x < kAwTable; ++x) g.norm.G[x] = g.step.G[x] = nullptr;
     for (int x = 0; x <= kAwTable; ++x) g.norm.start[x] = g.step.start[x] = 0;
     for (int x = 0; x < g.count; ++x) {
       const long long n = cfg.tensors[first + x].n;
-      g.norm.start[x] = g.chunks; g.step.start[x] = g.pieces;
+      g.step.start[x] = g.pieces;
       g.outer.push_back(g.blocks);
       g.chunks += (unsigned)cdiv(n, c->chunk);
       g.pieces += (unsigned)cdiv(n, c->piece);
       g.blocks += (unsigned)cdiv(n, kAwOuter);
     }
-    g.norm.start[g.count] = g.chunks; g.step.start[g.count] = g.pieces;
+    g.step.start[g.count] = g.pieces;
     g.outer.push_back(g.blocks);
     g.d_outer = reinterpret_cast<unsigned*>(take(4 * g.outer.size()));
     c->total_chunks += g.chunks;
@@ -164,8 +163,8 @@ size_t build(lordo_adamw_ctx* c, const lordo_adamw_buffers* buf, char* base) {
   return off;
 }
 
-AwLaunch launch_of(const lordo_adamw_ctx* c, const Group& g, unsigned units) {
-  return AwLaunch{c->d_tensors + g.first, g.count, c->cfg.K, units, c->cfg.w_dtype, c->cfg.g_dtype, c->cfg.states == LORDO_STATES_8BIT, c->piece};
+AwLaunch launch_of(const lordo_adamw_ctx* c, const Group& g, unsigned units, int piece) {
+  return AwLaunch{c->d_tensors + g.first, g.count, c->cfg.K, units, c->cfg.w_dtype, c->cfg.g_dtype, c->cfg.states == LORDO_STATES_8BIT, piece};
 }
 
 int check_launch(lordo_adamw_ctx* c, const char* what) {
@@ -218,9 +217,21 @@ int step(lordo_adamw_ctx* c, const lordo_grad* G, double lr, double beta1, doubl
   const float* coef = coef_dev;
   int stride = 0;
   if (!coef && cfg.clip_rho > 0.0) {
+    // a table whose gradient came by tokens has its sums of squares already: one chunk that adds them
+    unsigned total = 0;
     for (Group& g : c->groups) {
-      const AwClip clip = {c->d_partial, c->chunk, c->total_chunks, g.chunks_before, c->d_tickets, cfg.clip_rho, cfg.clip_scope, cfg.n_tensors, c->d_coef, c->d_status};
-      launch_aw_norm(launch_of(c, g, g.chunks), g.norm, clip, st);
+      g.chunks_before = total;
+      g.chunks = 0;
+      for (int x = 0; x < g.count; ++x) {
+        g.norm.start[x] = g.chunks;
+        g.chunks += G[g.first + x].tokens ? 1u : (unsigned)cdiv(c->tensors[g.first + x].n, c->chunk);
+      }
+      g.norm.start[g.count] = g.chunks;
+      total += g.chunks;
+    }
+    for (Group& g : c->groups) {
+      const AwClip clip = {c->d_partial, c->chunk, total, g.chunks_before, c->d_tickets, cfg.clip_rho, cfg.clip_scope, cfg.n_tensors, c->d_coef, c->d_status};
+      launch_aw_norm(launch_of(c, g, g.chunks, c->chunk), g.norm, clip, st);
       c->launches += 1;
     }
     coef = c->d_coef;
@@ -235,7 +246,7 @@ int step(lordo_adamw_ctx* c, const lordo_grad* G, double lr, double beta1, doubl
   a.root_inv_bc2 = (float)std::sqrt(1.0 / (1.0 - std::pow(cfg.beta2, (double)s)));
   a.key = stream_key(cfg.seed, 3, 0, s, 0);
   for (Group& g : c->groups) {
-    launch_aw_step(launch_of(c, g, g.pieces), g.step, coef, stride, a, st);
+    launch_aw_step(launch_of(c, g, g.pieces, c->piece), g.step, coef, stride, a, st);
     c->launches += 1;
   }
   rc = check_launch(c, "step");
@@ -301,7 +312,7 @@ int lordo_adamw_init(const lordo_adamw_config* cfg, const lordo_adamw_buffers* b
   for (Group& g : c->groups) ok = ok && cudaMemcpyAsync(g.d_outer, g.outer.data(), 4 * g.outer.size(), cudaMemcpyHostToDevice, st) == cudaSuccess;
   if (ok) {
     launch_fill_float(c->d_coef, (long long)cfg->n_tensors * cfg->K, 1.f, st);
-    for (Group& g : c->groups) launch_aw_init(launch_of(c, g, g.blocks), g.d_outer, st);
+    for (Group& g : c->groups) launch_aw_init(launch_of(c, g, g.blocks, kAwOuter), g.d_outer, st);
     c->launches += 1 + (int64_t)c->groups.size();
     ok = cudaStreamSynchronize(st) == cudaSuccess && cudaGetLastError() == cudaSuccess;
   }
@@ -332,7 +343,7 @@ int lordo_adamw_outer_step(lordo_adamw_ctx* c, void* stream) {
   const AwOuter o = {c->cfg.sync_m, c->cfg.sync_v, c->cfg.outer == LORDO_OUTER_NESTEROV, (float)c->cfg.outer_lr, (float)c->cfg.outer_momentum,
                      stream_key(c->cfg.seed, 4, 0, c->outers, 0)};
   for (Group& g : c->groups) {
-    launch_aw_outer(launch_of(c, g, g.blocks), g.d_outer, o, st);
+    launch_aw_outer(launch_of(c, g, g.blocks, kAwOuter), g.d_outer, o, st);
     c->launches += 1;
   }
   rc = check_launch(c, "outer");

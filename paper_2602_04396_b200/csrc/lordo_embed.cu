@@ -435,18 +435,19 @@ __device__ __forceinline__ void window_sums(const SumArgs& a, int k, int w, long
   float acc[VEC] = {};
   float* part = a.parts + ((long long)k * a.windows + w) * 2 * a.d + col;
   const long long first = (long long)k * a.T * a.d + (on ? col : 0);
-  for (int b = 0; b < n; b += kAhead) {
-    Piece<DT, VEC> x[kAhead];
-    Old<ODT, VEC> old[kAhead];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      const int pos = __shfl_sync(0xffffffffu, mine.y, (b + j) & 31);
-      if (b + j < n && on) x[j].load(a.dY, first + (long long)pos * a.d);
-      if (MODE == SUM_ADD) {
-        const int v = __shfl_sync(0xffffffffu, mine.x, (b + j) & 31);
-        if (on && ((ends >> ((b + j) & 31)) & 1u)) old[j].load(a.out, ((long long)k * a.V + v) * a.d + col);
-      }
+  Piece<DT, VEC> x[kAhead];
+  Old<ODT, VEC> old[kAhead];
+  auto fetch = [&](int i, Piece<DT, VEC>& row, Old<ODT, VEC>& was) {  // entry i of the window; every lane is here
+    const int pos = __shfl_sync(0xffffffffu, mine.y, i & 31);
+    if (i < n && on) row.load(a.dY, first + (long long)pos * a.d);
+    if (MODE == SUM_ADD) {
+      const int v = __shfl_sync(0xffffffffu, mine.x, i & 31);
+      if (i < n && on && ((ends >> (i & 31)) & 1u)) was.load(a.out, ((long long)k * a.V + v) * a.d + col);
     }
+  };
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) fetch(j, x[j], old[j]);
+  for (int b = 0; b < n; b += kAhead) {
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       if (b + j >= n) break;
@@ -466,6 +467,7 @@ __device__ __forceinline__ void window_sums(const SumArgs& a, int k, int w, long
         came_in = false;
         start = s + b + j + 1;
       }
+      fetch(b + j + kAhead, x[j], old[j]);
     }
   }
   if (!((ends >> (n - 1)) & 1u) && on) {
