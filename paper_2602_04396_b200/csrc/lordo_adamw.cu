@@ -326,14 +326,17 @@ __device__ __forceinline__ unsigned pack8(const float2 (&x)[2], float inv, const
 }
 
 // sqrt(v) by one of Newton's (Heron's) steps on r^2 = v from r = v rsqrt(v), whose derivative 2 r is 2 / rsqrt(v): of normal numbers off by less than
-// a unit in the last place, as a rule rounded to the nearest. The step is not a number for 0 (and below 2^-126), infinity and NaN; the maximum
-// then takes v 1e-20, which is 0, infinity and NaN, and below the root of any other v. No branch; sqrtf has one.
+// a unit in the last place, as a rule rounded to the nearest. The step is not a number for 0 (and below 2^-126), infinity and NaN; there, unless
+// all are NORMAL, the maximum takes v 1e-20, which is 0, infinity and NaN, and below the root of any other v. No branch; sqrtf has one.
+template <bool NORMAL>
 __device__ __forceinline__ float2 root(float2 v) {
   float2 y;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(v.x));
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(v.y));
   const float2 r = __fmul2_rn(v, y), minus = __fmul2_rn(v, make_float2(-y.x, -y.y));
-  const float2 x = __ffma2_rn(__ffma2_rn(minus, r, v), __fmul2_rn(y, make_float2(0.5f, 0.5f)), r), least = __fmul2_rn(v, make_float2(1e-20f, 1e-20f));
+  const float2 x = __ffma2_rn(__ffma2_rn(minus, r, v), __fmul2_rn(y, make_float2(0.5f, 0.5f)), r);
+  if (NORMAL) return x;
+  const float2 least = __fmul2_rn(v, make_float2(1e-20f, 1e-20f));
   return make_float2(fmaxf(x.x, least.x), fmaxf(x.y, least.y));
 }
 __device__ __forceinline__ float reciprocal(float x) {
@@ -348,15 +351,41 @@ struct Step8 {  // constants of a step, of its worker and tensor
 
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
+// What follows the moments: roots, weights, codes of a lane's eight elements. v becomes its codes in vc. NORMAL: every v is a normal number whose root
+// is at least the smallest code, and scales are below 2^7.
+template <bool NORMAL, bool QHM>
+__device__ __forceinline__ void finish8(const Step8& s, unsigned long long counter, const float2 (&g)[4], const float2 (&m)[4], const float2 (&v)[4],
+                                        float2 (&w)[4], unsigned (&mc)[2], unsigned (&vc)[2], float mi, float vi) {
+  const float2 lm = both(-s.lm), lg = both(-s.lg * s.c), keep = both(s.keep), q = both(s.root_inv_bc2), eps = both(s.eps);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const unsigned long long x = mix64(counter + h * kGolden);
+    unsigned u[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[j] = first16(x, j);
+    const float2 mh[2] = {m[2 * h], m[2 * h + 1]}, rh[2] = {root<NORMAL>(v[2 * h]), root<NORMAL>(v[2 * h + 1])};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int at = 2 * h + j;
+      const float2 d = __ffma2_rn(rh[j], q, eps);
+      float2 up = __fmul2_rn(lm, mh[j]);
+      if (QHM) up = __ffma2_rn(lg, g[at], up);
+      w[at] = __ffma2_rn(up, make_float2(reciprocal(d.x), reciprocal(d.y)), __fmul2_rn(w[at], keep));
+    }
+    mc[h] = NORMAL ? pack8<PACK_SIGNED, false>(mh, mi * 0x1p-120f, u) : pack8<PACK_ANY, false>(mh, mi, u);
+    vc[h] = NORMAL ? pack8<PACK_POSITIVE, true>(rh, vi * 0x1p-120f, u) : pack8<PACK_ANY, true>(rh, vi, u);
+  }
+}
+
 // A lane's eight elements of a block of 256 of one worker's tensor: codes in, codes and scales out. Arithmetic goes by pairs of elements in one
 // instruction each (the issue slots are what a step is short of), every product and sum rounded on its own. The scales are powers of two, so that
 // b1 (m8 S) is (b1 S) m8 to the last bit, and b2 (s8 S)^2 is (b2 S^2) s8^2. The weights' quotient is good to two units in the last place.
+template <bool QHM>
 __device__ __forceinline__ void step8_lane(const Step8& s, unsigned long long counter, const float2 (&g)[4], float2 (&w)[4], unsigned (&mc)[2],
                                            unsigned (&vc)[2], int& mcode, int& vcode) {
   const float ms = pow2(mcode), vs = pow2(vcode);
   const float2 b1 = both(s.b1 * ms), b2 = both(s.b2 * (vs * vs)), c = both(s.c), a1 = both(s.a1), a2 = both(s.a2);
-  const float2 lm = both(-s.lm), lg = both(-s.lg), keep = both(s.keep), q = both(s.root_inv_bc2), eps = both(s.eps);
-  float2 m[4], r[4];
+  float2 m[4], v[4];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     float2 x[2], y[2];
@@ -367,32 +396,26 @@ __device__ __forceinline__ void step8_lane(const Step8& s, unsigned long long co
       const int at = 2 * h + j;
       const float2 z = __fmul2_rn(g[at], c);
       m[at] = __fadd2_rn(__fmul2_rn(b1, x[j]), __fmul2_rn(a1, z));
-      r[at] = root(__fadd2_rn(__fmul2_rn(b2, __fmul2_rn(y[j], y[j])), __fmul2_rn(__fmul2_rn(a2, z), z)));
-      const float2 d = __ffma2_rn(r[at], q, eps);
-      w[at] = __ffma2_rn(__ffma2_rn(lm, m[at], __fmul2_rn(lg, z)), make_float2(reciprocal(d.x), reciprocal(d.y)), __fmul2_rn(w[at], keep));
+      v[at] = __fadd2_rn(__fmul2_rn(b2, __fmul2_rn(y[j], y[j])), __fmul2_rn(__fmul2_rn(a2, z), z));
     }
   }
-  const unsigned mtop = __reduce_max_sync(0xffffffffu, top_signed(m)), vtop = __reduce_max_sync(0xffffffffu, top_positive(r));
+  const unsigned mtop = __reduce_max_sync(0xffffffffu, top_signed(m)), vtop = __reduce_max_sync(0xffffffffu, top_positive(v));
+  const float rtop = root<false>(both(__uint_as_float(vtop))).x;
   mcode = scale_code(mtop);
-  vcode = scale_code(vtop);
-  // scales above 2^6 (their reciprocal's 2^-120 would not be a normal number), infinities, NaN; and sqrt(v) of 0 or below half the smallest code
-  constexpr unsigned kLarge = (127u + 14u) << 23;
+  vcode = scale_code(__float_as_uint(rtop));
   const float mi = pow2(254 - mcode), vi = pow2(254 - vcode);
-  const bool slow = mtop >= kLarge || vtop >= kLarge || __any_sync(0xffffffffu, __uint_as_float(low_positive(r)) * vi < 0x1p-9f);
+  // scales above 2^6 (their reciprocal's 2^-120 would not be a normal number), infinities, NaN; v whose root is below the smallest code, or not normal
+  constexpr unsigned kLarge = (127u + 14u) << 23;
+  const float least = fmaxf(0x1p-18f * (pow2(vcode) * pow2(vcode)), 0x1p-126f);
+  const bool slow = mtop >= kLarge || __float_as_uint(rtop) >= kLarge || __any_sync(0xffffffffu, __uint_as_float(low_positive(v)) < least);
+  if (!slow) {
+    finish8<true, QHM>(s, counter, g, m, v, w, mc, vc, mi, vi);
+  } else if (mtop | vtop) {
+    finish8<false, QHM>(s, counter, g, m, v, w, mc, vc, mi, vi);
+  } else {  // a block that never had a gradient
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const unsigned long long x = mix64(counter + h * kGolden);
-    unsigned u[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) u[j] = first16(x, j);
-    const float2 mh[2] = {m[2 * h], m[2 * h + 1]}, rh[2] = {r[2 * h], r[2 * h + 1]};
-    if (slow) {
-      mc[h] = pack8<PACK_ANY, false>(mh, mi, u);
-      vc[h] = pack8<PACK_ANY, true>(rh, vi, u);
-    } else {
-      mc[h] = pack8<PACK_SIGNED, false>(mh, mi * 0x1p-120f, u);
-      vc[h] = pack8<PACK_POSITIVE, true>(rh, vi * 0x1p-120f, u);
-    }
+    for (int j = 0; j < 4; ++j) w[j] = __fmul2_rn(w[j], both(s.keep));
+    mc[0] = mc[1] = vc[0] = vc[1] = 0u;
   }
 }
 
@@ -444,7 +467,7 @@ __device__ __forceinline__ void put8(char* to, const float2 (&x)[4]) {
 // warp's ring in shared memory, some blocks ahead; no other lane touches that.
 // ROWS: the gradient is in rows that were summed by token (fp32); which row a lane wants of a block is looked up a block ahead of the copies.
 constexpr int kRing8 = 48 * 1024;
-template <int WDT, int GDT, bool ROWS>
+template <int WDT, int GDT, bool ROWS, bool QHM>
 __device__ __forceinline__ void step8_blocks(const AwTensor& T, const Arrays8& a, const Step8& s, unsigned long long key, long long b0, long long b1, int lane, int warp, char* ring) {
   constexpr int kWb = WDT == LORDO_F32 ? 4 : 2, kGb = GDT == LORDO_F32 ? 4 : 2, kStep = 8 * kAwBlock;  // elements from block to block
   constexpr int kM = 256 * (kWb + kGb), kStage = kM + 512, kStages = kRing8 / 8 / kStage;
@@ -507,7 +530,7 @@ __device__ __forceinline__ void step8_blocks(const AwTensor& T, const Arrays8& a
     const uint2 y = *reinterpret_cast<const uint2*>(p + kM - 8 * lane), z = *reinterpret_cast<const uint2*>(p + kM + 256 - 8 * lane);
     unsigned mc[2] = {y.x, y.y}, vc[2] = {z.x, z.y};
     int mcode = __shfl_sync(0xffffffffu, mcodes, x), vcode = __shfl_sync(0xffffffffu, vcodes, x);
-    step8_lane(s, counter, g, w, mc, vc, mcode, vcode);
+    step8_lane<QHM>(s, counter, g, w, mc, vc, mcode, vcode);
     constexpr int kBack = (kStages - 1) * kStep;
     put8<WDT>(pw - kBack * kWb, w);
     *reinterpret_cast<uint2*>(pm - kBack) = make_uint2(mc[0], mc[1]);
@@ -527,7 +550,7 @@ __device__ __forceinline__ void step8_blocks(const AwTensor& T, const Arrays8& a
   }
 }
 
-template <int WDT, int GDT>
+template <int WDT, int GDT, bool QHM>
 __global__ void __launch_bounds__(256, 4) adamw_step8_kernel(const __grid_constant__ AwTable tab, AwLaunch l, const float* __restrict__ coef, int stride, AwStep a) {
   __shared__ __align__(16) char ring[kRing8];
   const int lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);  // the compiler sees that a warp has one
@@ -556,8 +579,8 @@ __global__ void __launch_bounds__(256, 4) adamw_step8_kernel(const __grid_consta
   x.rows = T.rows + (long long)k * T.cap * T.d;
   if ((base & 7) == 0 && (G || T.row_mul)) {
     const long long whole = T.n / kAwBlock < b1 ? T.n / kAwBlock : b1;
-    if (G) step8_blocks<WDT, GDT, false>(T, x, s, key, b0, whole, lane, warp, ring);
-    else step8_blocks<WDT, LORDO_F32, true>(T, x, s, key, b0, whole, lane, warp, ring);
+    if (G) step8_blocks<WDT, GDT, false, QHM>(T, x, s, key, b0, whole, lane, warp, ring);
+    else step8_blocks<WDT, LORDO_F32, true, QHM>(T, x, s, key, b0, whole, lane, warp, ring);
     b0 = whole > b0 ? whole : b0;
   }
   // the last block of a worker, workers whose arrays begin at odd addresses, gradients by tokens
@@ -590,7 +613,7 @@ __global__ void __launch_bounds__(256, 4) adamw_step8_kernel(const __grid_consta
       g[j] = make_float2(ge[2 * j], ge[2 * j + 1]);
       w[j] = make_float2(we[2 * j], we[2 * j + 1]);
     }
-    step8_lane(s, counter4(key, e), g, w, mc, vc, mcode, vcode);
+    step8_lane<QHM>(s, counter4(key, e), g, w, mc, vc, mcode, vcode);
     if (vec) {
       put8<WDT>(reinterpret_cast<char*>(x.W) + e * (WDT == LORDO_F32 ? 4 : 2), w);
       *reinterpret_cast<uint2*>(x.m + e) = make_uint2(mc[0], mc[1]);
@@ -764,7 +787,7 @@ __device__ __forceinline__ void outer_mean8(const AwTensor& T, int K, float inv_
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     a[j] = __fmul2_rn(a[j], both(inv_k));
-    if (SECOND) a[j] = root(a[j]);
+    if (SECOND) a[j] = root<false>(a[j]);
   }
   const int code = scale_code(__reduce_max_sync(0xffffffffu, SECOND ? top_positive(a) : top_signed(a)));
   const float inv = pow2(254 - code);
@@ -849,7 +872,8 @@ void launch_aw_norm(const AwLaunch& l, const AwTable& t, const AwClip& c, cudaSt
 void launch_aw_step(const AwLaunch& l, const AwTable& t, const float* coef, int stride, const AwStep& s, cudaStream_t st) {
   const dim3 grid(l.units * (unsigned)l.K);
 #define LORDO_AW(W, G)                                                                              \
-  if (l.small) launch_dep(adamw_step8_kernel<W, G>, grid, 256, 0, st, t, l, coef, stride, s);       \
+  if (l.small && s.a_omega != 0.f) launch_dep(adamw_step8_kernel<W, G, true>, grid, 256, 0, st, t, l, coef, stride, s);  \
+  else if (l.small) launch_dep(adamw_step8_kernel<W, G, false>, grid, 256, 0, st, t, l, coef, stride, s);                \
   else launch_dep(adamw_step_kernel<W, G>, grid, 256, 0, st, t, l, coef, stride, s)
   if (l.w_dt == LORDO_F32) {
     if (l.g_dt == LORDO_F32) { LORDO_AW(LORDO_F32, LORDO_F32); } else { LORDO_AW(LORDO_F32, LORDO_BF16); }
