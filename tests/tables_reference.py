@@ -70,10 +70,11 @@ def round8(x: np.ndarray, u: np.ndarray, positive: bool):
     return np.copysign(q, x), e, np.abs(y - np.rint(y))
 
 
-def adamw(W, m, v, g, lr, beta1, beta2, omega, eps, wd, s):
-    """One step in 64 bits: (W, m, v, size of the update before lr)."""
+def adamw(W, m, v, g, lr, beta1, beta2, omega, eps, wd, s, least=0.0):
+    """One step in 64 bits: (W, m, v, size of the update before lr). least: below this v counts as 0."""
     m = beta1 * m + (1 - beta1) * g
     v = beta2 * v + (1 - beta2) * g * g
+    v = np.where(v < least, 0.0, v)
     up = (omega * m / (1 - beta1 ** s) + (1 - omega) * g) / (np.sqrt(v / (1 - beta2 ** s)) + eps)
     return W - lr * (up + wd * W), m, v, up
 

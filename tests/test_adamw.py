@@ -189,6 +189,108 @@ def test_steps(name, w, g, states, K, rho, scope, omega):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("std", [1e-14, 1e-6, 30.0, 1e6])
+@pytest.mark.parametrize("kind", ["spread", "half empty", "one"])
+def test_magnitudes_in_8_bits(std, kind):
+    """Two steps on gradients from far below to far above 1: blocks whose magnitudes lie 30 powers of two apart, blocks with rows that never had a
+    gradient beside others, blocks with one element that had. Checked as the other steps are.
+
+    v is formed in fp32 and counts as 0 below 2^-126, the smallest normal number: gradients of 1e-14 * 2^-30 have squares of 1e-46, which fp32 does
+    not hold. Its operands may be subnormal, each off by 2^-150: of a v at 2^-126 that is 2^-23, so v within 1e-6 of that border may go either way."""
+    K, n = 2, 256 * 40 + 24
+    least = 2.0 ** -126
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    opt = adamw.AdamW([torch.ones(n)], K, states="8bit", beta2=0.99, eps=std * 1e-3, seed=21)
+    W0 = ref.to64(opt.W[0])
+    m0 = v0 = np.zeros((K, n))
+    for s in range(1, 3):
+        g = torch.randn(K, n, device="cuda", generator=gen) * std
+        if kind == "spread":
+            g *= torch.exp2(-30.0 * torch.rand(K, n, device="cuda", generator=gen))
+        elif kind == "half empty":
+            g[:, (torch.arange(n, device="cuda") // 100) % 2 == 0] = 0.0
+        else:
+            g[:, torch.arange(n, device="cuda") % 300 != 7] = 0.0
+        opt.step([g], 0.01, 0.9)
+        G = ref.to64(g)
+        raw = 0.99 * v0 + 0.01 * G * G
+        assert not (np.abs(raw / least - 1) < 1e-6).any()  # none at the border among these
+        W, m, v, up = ref.adamw(W0, m0, v0, G, 0.01, 0.9, 0.99, 1.0, std * 1e-3, 0.0, s, least=least)
+        dm = 4 * HALF["f32"] * (np.abs(0.9 * m0) + np.abs(0.1 * G))
+        u = [ref.random16(21, 3, s, k, n) for k in range(K)]
+        check_moments8(opt.m[0], opt.ms[0], m, dm + 4 * HALF["f32"] * np.abs(m), u, False)
+        check_moments8(opt.v[0], opt.vs[0], np.sqrt(v), 8 * HALF["f32"] * np.sqrt(v), [ref.second16(x) for x in u], True)
+        got = ref.to64(opt.W[0])
+        D = np.sqrt(v / (1 - 0.99 ** s)) + std * 1e-3
+        off = 0.01 * (dm / (1 - 0.9 ** s) / D + 16 * HALF["f32"] * np.abs(up)) + 2 * HALF["f32"] * np.abs(W)
+        assert (np.abs(got - W) <= off).all()
+        assert torch.equal(opt.v[0].float() != 0, torch.from_numpy(v != 0).cuda())  # what had a gradient never comes to 0, the rest is
+        wide = lambda c, sc: ref.to64(c) * np.repeat(ref.to64(sc), 256, axis=1)[:, :n]
+        W0, m0, v0 = got, wide(opt.m[0], opt.ms[0]), wide(opt.v[0], opt.vs[0]) ** 2
+    opt.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("states", ["f32", "8bit"])
+def test_two_tables_by_tokens_and_many_workers(states):
+    """Token and position tables in one step, fewer tokens than declared, 64 workers; then the same step with dense gradients for one of them:
+    coefficients as for the dense gradients (test_norm_of_a_gradient_by_tokens derives their bound), the rest from outside."""
+    from paper_2602_04396_b200 import embedding
+    K = 64
+    shapes = [(40, 24), (33,), (16, 24)]
+    a = group(shapes, K, 1, states=states, tables={0: 50, 2: 16}, clip_rho=0.5, seed=4)
+    b = group(shapes, K, 1, states=states, clip_rho=0.5, seed=4)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    for s in range(2):
+        tok = torch.randint(0, 40, (K, 2, 8), device="cuda", generator=gen)
+        pos = torch.arange(16, device="cuda").view(1, 2, 8).expand(K, 2, 8).contiguous()
+        dY = torch.randn(K, 2, 8, 24, device="cuda", generator=gen)
+        g1 = gradients([(33,)], K, s, "f32")[0]
+        dense = [embedding.embedding_grad(dY, x, n, K=K) for x, n in ((tok, 40), (pos, 16))]
+        a.step([adamw.TokenGrad(tok, dY), g1, adamw.TokenGrad(pos, dY)], 0.01)
+        b.step([dense[0], g1, dense[1]], 0.01)
+        ca, cb = ref.to64(a.clip_coefficients()), ref.to64(b.clip_coefficients())
+        assert (np.abs(ca - cb) <= (2 * COEF + 40 * 2.0 ** -24) * cb).all()
+        coef = torch.rand(K, device="cuda", generator=gen)
+        a.step([adamw.TokenGrad(tok, dY), g1, dense[1]], 0.01, coef=coef)
+        b.step([dense[0], g1, dense[1]], 0.01, coef=coef)
+    c = group(shapes, K, 1, states=states, tables={0: 50, 2: 16}, seed=4)
+    d = group(shapes, K, 1, states=states, seed=4)
+    c.step([adamw.TokenGrad(tok, dY), g1, adamw.TokenGrad(pos, dY)], 0.01)
+    d.step([dense[0], g1, dense[1]], 0.01)
+    for x in c.storage:
+        assert torch.equal(c.storage[x].view(torch.uint8), d.storage[x].view(torch.uint8)), x
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("states", ["f32", "8bit"])
+def test_elements_behind_two_to_the_32nd(states):
+    """Two workers of 2^31 + 24 elements each (and a small tensor behind them): the last ones move as those of a small group with the same
+    gradients, bit for bit where rounding does not look at the element's number, and the synchronisation reaches them."""
+    n, tail = 2 ** 31 + 24, 24
+    K = 2
+    big = adamw.AdamW([torch.zeros(n, dtype=torch.bfloat16), torch.zeros(9, dtype=torch.bfloat16)], K, states=states, outer=lordo.OUTER_AVG)
+    small = adamw.AdamW([torch.zeros(tail, dtype=torch.bfloat16), torch.zeros(9, dtype=torch.bfloat16)], K, states=states, outer=lordo.OUTER_AVG)
+    G = [torch.zeros(K, n, device="cuda", dtype=torch.bfloat16), torch.ones(K, 9, device="cuda", dtype=torch.bfloat16)]
+    g = torch.randn(K, tail, device="cuda").to(torch.bfloat16)
+    G[0][:, -tail:] = g
+    coef = torch.ones(K, device="cuda")
+    big.step(G, 0.1, coef=coef)
+    small.step([g, G[1]], 0.1, coef=coef)
+    assert torch.equal(big.W[0][:, -tail:], small.W[0]) and torch.equal(big.W[1], small.W[1])
+    assert not big.W[0][:, n // 2:n // 2 + 1000].any() and not big.W[0][:, :1000].any()
+    if states == "f32":
+        assert torch.equal(big.m[0][:, -tail:], small.m[0]) and torch.equal(big.v[0][:, -tail:], small.v[0])
+    else:  # one block of 24 elements in either
+        assert torch.equal(big.ms[0][:, -1].float(), small.ms[0][:, -1].float())
+        assert (big.v[0][:, -tail:].float() > 0).all() and not big.v[0][:, -tail - 1000:-tail].view(torch.uint8).any()
+    big.outer_step()
+    small.outer_step()
+    assert torch.equal(big.W[0][:, -tail:], small.W[0])
+    big.close(), small.close()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("V,d,T", [(50, 8, 1), (300, 40, 700), (97, 33, 64), (5, 16, 3000), (3000, 264, 33), (700, 128, 0)])
 @pytest.mark.parametrize("states", ["f32", "8bit"])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])

@@ -189,6 +189,24 @@ def test_empty_batches():
 
 
 @pytest.mark.gpu
+def test_rows_behind_two_to_the_32nd():
+    """A table of 8 x 70001 x 8192 elements (9.2 GB): rows at its end, read and added to."""
+    K, V, d = 8, 70001, 8192
+    W = torch.zeros(K, V, d, device="cuda", dtype=torch.bfloat16)
+    W[K - 1, V - 1] = torch.randn(d, device="cuda").to(torch.bfloat16)
+    tok = torch.full((K, 40), V - 1, device="cuda", dtype=torch.int32)
+    tok[:, ::3] = 0
+    out = embedding.embedding(W, tok)
+    assert torch.equal(out[K - 1, 1], W[K - 1, V - 1]) and not out[:K - 1].any() and not out[:, 0].any()
+    dY = torch.ones(K, 40, d, device="cuda", dtype=torch.bfloat16)
+    was = W[K - 1, V - 1].clone()
+    embedding.embedding_grad(dY, tok, V, out=W, accumulate=True)
+    assert torch.equal(W[K - 1, V - 1], (was.float() + 26.0).to(torch.bfloat16)) and (W[K - 1, 0] == 14).all() and not W[:, 1:V - 1].any()
+    embedding.embedding_grad(dY, tok, V, out=W)
+    assert (W[:, V - 1] == 26).all() and (W[:, 0] == 14).all() and not W[:, 1:V - 1].any()
+
+
+@pytest.mark.gpu
 def test_streams_and_graphs():
     """On a stream of its own, and captured twice and replayed in turn on other inputs: the eager call's bits."""
     V, T = 700, 5000
