@@ -346,7 +346,7 @@ __device__ __forceinline__ float reciprocal(float x) {
 }
 
 struct Step8 {  // constants of a step, of its worker and tensor
-  float c, b1, a1, b2, a2, keep, lm, lg, root_inv_bc2, eps;
+  float one, c, b1, a1, b2, a2, keep, lm, lg, root_inv_bc2, eps;
 };
 
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
@@ -378,13 +378,14 @@ __device__ __forceinline__ void finish8(const Step8& s, unsigned long long count
 }
 
 // A lane's eight elements of a block of 256 of one worker's tensor: codes in, codes and scales out. Arithmetic goes by pairs of elements in one
-// instruction each (the issue slots are what a step is short of), every product and sum rounded on its own. The scales are powers of two, so that
+// instruction each (the issue slots are what a step is short of), every product and sum of the moments rounded on its own: a sum is p times one
+// plus q, because nvcc 12.9 fuses a packed product with a packed sum that takes it, mul.rn.f32x2 with add.rn.f32x2 too. The scales are powers of two, so that
 // b1 (m8 S) is (b1 S) m8 to the last bit, and b2 (s8 S)^2 is (b2 S^2) s8^2. The weights' quotient is good to two units in the last place.
 template <bool QHM>
 __device__ __forceinline__ void step8_lane(const Step8& s, unsigned long long counter, const float2 (&g)[4], float2 (&w)[4], unsigned (&mc)[2],
                                            unsigned (&vc)[2], int& mcode, int& vcode) {
   const float ms = pow2(mcode), vs = pow2(vcode);
-  const float2 b1 = both(s.b1 * ms), b2 = both(s.b2 * (vs * vs)), c = both(s.c), a1 = both(s.a1), a2 = both(s.a2);
+  const float2 b1 = both(s.b1 * ms), b2 = both(s.b2 * (vs * vs)), c = both(s.c), a1 = both(s.a1), a2 = both(s.a2), one = both(s.one);
   float2 m[4], v[4];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -395,8 +396,8 @@ __device__ __forceinline__ void step8_lane(const Step8& s, unsigned long long co
     for (int j = 0; j < 2; ++j) {
       const int at = 2 * h + j;
       const float2 z = __fmul2_rn(g[at], c);
-      m[at] = __fadd2_rn(__fmul2_rn(b1, x[j]), __fmul2_rn(a1, z));
-      v[at] = __fadd2_rn(__fmul2_rn(b2, __fmul2_rn(y[j], y[j])), __fmul2_rn(__fmul2_rn(a2, z), z));
+      m[at] = __ffma2_rn(__fmul2_rn(b1, x[j]), one, __fmul2_rn(a1, z));
+      v[at] = __ffma2_rn(__fmul2_rn(b2, __fmul2_rn(y[j], y[j])), one, __fmul2_rn(__fmul2_rn(a2, z), z));
     }
   }
   const unsigned mtop = __reduce_max_sync(0xffffffffu, top_signed(m)), vtop = __reduce_max_sync(0xffffffffu, top_positive(v));
@@ -561,7 +562,7 @@ __global__ void __launch_bounds__(256, 4) adamw_step8_kernel(const __grid_consta
   const void* G = tab.G[i];
   const unsigned long long key = mix64(a.key + kGolden * ((unsigned long long)T.index * l.K + k + 1));
   Step8 s;
-  s.b1 = a.b1; s.a1 = a.a1; s.b2 = a.b2; s.a2 = a.a2; s.root_inv_bc2 = a.root_inv_bc2; s.eps = a.eps;
+  s.one = a.one; s.b1 = a.b1; s.a1 = a.a1; s.b2 = a.b2; s.a2 = a.a2; s.root_inv_bc2 = a.root_inv_bc2; s.eps = a.eps;
   s.keep = 1.f - a.lr * T.wd; s.lm = a.lr * a.omega * a.inv_bc1; s.lg = a.lr * a.a_omega;
   dep_begin();
   s.c = coef ? __ldcg(coef + (long long)T.index * stride + k) : 1.f;

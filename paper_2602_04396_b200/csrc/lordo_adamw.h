@@ -30,7 +30,7 @@ struct AwTensor {
   const float* rows;       // [K][cap][d] sums, at the first sorted entry of their token
   const double* rowsq;     // [K][rowsq_count] sums of their squares
   const int* rowsq_count;
-  // rows of eighths of d: x / (d / 8) = (x * row_mul) >> (31 + row_shift) for x < 2^31; row_mul = 0 where d is no multiple of 8 or n too large
+  // divides by d / 8 (lordo_plan.h); row_mul = 0 where d is no multiple of 8 or n too large
   unsigned row_mul;
   int row_shift;
 };
@@ -45,6 +45,7 @@ struct AwStep {
   float lr, b1, a1, b2, a2;  // a = 1 - b
   float omega, a_omega, eps;
   float inv_bc1, inv_bc2, root_inv_bc2;
+  float one;                 // 1, as a number that the compiler does not know
   unsigned long long key;    // of the rounding, for this step
 };
 

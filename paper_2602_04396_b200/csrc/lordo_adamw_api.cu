@@ -151,10 +151,10 @@ size_t build(lordo_adamw_ctx* c, const lordo_adamw_buffers* buf, char* base) {
       tb.rows.sq = reinterpret_cast<double*>(take(8 * (size_t)K * tok_row_blocks_max(t.max_tokens, t.row)));
       tb.rows.count = reinterpret_cast<int*>(take(4));
       tb.rows.cap = t.max_tokens;
-      if (t.row % 8 == 0 && t.n / 8 < (1ll << 31)) {  // the multiplier is at most 2^32 - 1, and off by less than 2^row_shift / 2^(31 + row_shift) of the quotient
-        const unsigned long long eighths = (unsigned long long)t.row / 8;
-        while ((1ull << a.row_shift) < eighths) a.row_shift += 1;
-        a.row_mul = (unsigned)((1ull << (31 + a.row_shift)) / eighths + 1);
+      if (t.row % 8 == 0 && t.n / 8 < (1ll << 31)) {
+        const Divider by = divider((unsigned)(t.row / 8));
+        a.row_mul = by.mul;
+        a.row_shift = by.shift;
       }
       a.segs = tb.scratch.segs; a.rows = tb.rows.rows; a.rowsq = tb.rows.sq; a.rowsq_count = tb.rows.count;
       c->tables.push_back(tb);
@@ -244,6 +244,7 @@ int step(lordo_adamw_ctx* c, const lordo_grad* G, double lr, double beta1, doubl
   a.inv_bc1 = (float)(1.0 / (1.0 - std::pow(beta1, (double)s)));
   a.inv_bc2 = (float)(1.0 / (1.0 - std::pow(cfg.beta2, (double)s)));
   a.root_inv_bc2 = (float)std::sqrt(1.0 / (1.0 - std::pow(cfg.beta2, (double)s)));
+  a.one = 1.f;
   a.key = stream_key(cfg.seed, 3, 0, s, 0);
   for (Group& g : c->groups) {
     launch_aw_step(launch_of(c, g, g.pieces, c->piece), g.step, coef, stride, a, st);

@@ -12,6 +12,19 @@ namespace lordo {
 // fewer at hand the same ranges and chunks take more waves. Lists that lordo_init alone makes go by the device's own count.
 constexpr int kPlannedSms = 148;
 
+// Division by a constant q >= 1 (at most 2^24) of any x < 2^31: x / q = (x * mul) >> (31 + shift). With 2^shift the power of two not below q and mul the next
+// whole number above 2^(31 + shift) / q, mul q is at most q <= 2^shift too large, so x mul / 2^(31 + shift) is less than 1 / q above x / q.
+struct Divider {
+  unsigned mul;
+  int shift;
+};
+inline Divider divider(unsigned q) {
+  Divider d = {0u, 0};
+  while ((1ull << d.shift) < q) d.shift += 1;
+  d.mul = (unsigned)((1ull << (31 + d.shift)) / q + 1);
+  return d;
+}
+
 // Ranges of k that a product of the refresh with few output tiles is dealt out in: the count with the shortest last wave on
 // `pairs` CTA pairs, a range costing about four steps of 64 k on top of its own (start of the pipeline, epilogue), and
 // left four steps at least. A range has at most 64 steps, whatever their count: the tensor cores' fp32 accumulation truncates, and

@@ -1,5 +1,6 @@
 """AdamW groups (parameters outside the low-rank path) against the plain numpy forms."""
 import ctypes as C
+import subprocess
 
 import numpy as np
 import pytest
@@ -79,6 +80,22 @@ def test_configurations_are_checked(lib):
     # a table's scratch: the sums of up to 50 rows of 10 for both workers
     assert query(((100, 10, 50, 0.0),)) >= plain + 4 * 2 * 50 * 10
     assert lib.lordo_adamw_query_workspace(None, None) == 1
+
+
+def test_division_by_multiplication(tmp_path):
+    """The rule by which a step finds the row of an element (csrc/lordo_plan.h): at multiples of the divisor, beside them and at the ends."""
+    src, so = str(tmp_path / "d.cpp"), str(tmp_path / "d.so")
+    with open(src, "w") as f:
+        f.write('#include "lordo_plan.h"\nextern "C" unsigned quotient(unsigned x, unsigned q) {\n  const lordo::Divider d = lordo::divider(q);\n'
+                '  return (unsigned)(((unsigned long long)x * d.mul) >> (31 + d.shift));\n}\n')
+    subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I", lbuild.CSRC, "-o", so, src], check=True)
+    f = C.CDLL(so).quotient
+    f.restype, f.argtypes = C.c_uint, [C.c_uint, C.c_uint]
+    rng = np.random.default_rng(0)
+    for q in [1, 2, 3, 5, 7, 96, 125, 256, 1000, 2 ** 20 - 1, 2 ** 20, 2 ** 20 + 1, 2 ** 21 - 1, 2 ** 24 - 1, 2 ** 24] + rng.integers(1, 2 ** 21, 200).tolist():
+        k = rng.integers(0, (2 ** 31 - 2) // q + 1, 40)
+        for x in [0, q - 1, q, 2 ** 31 - 1, 2 ** 31 - 2] + (k * q).tolist() + np.maximum(k * q - 1, 0).tolist():
+            assert f(x, q) == x // q, (x, q)
 
 
 def test_null_arguments_are_rejected(lib):
