@@ -12,8 +12,8 @@ from tests import tables_reference as ref
 
 DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}  # half a step, relative
-# A worker's gradient norm is a sum of squares: a thread adds up to 64 of them one after another in fp32 (relative 64 half steps of the sum), the
-# rest is fp64; its root halves that, and the coefficient adds a few roundings.
+# A worker's gradient norm is a sum of squares: a thread adds eight of them one after another in fp32 (relative 8 half steps of the sum, 64 of
+# them would be covered too), the rest is fp64; its root halves that, and the coefficient adds a rounding.
 COEF = 40 * 2.0 ** -24
 
 
