@@ -368,7 +368,8 @@ typedef struct {
  * was added, u being 16 bits of the generator behind lordo_fill_random for (seed, step, tensor, worker, element): the expected value
  * is the exact one, so averages with beta near 1, whose change in a step is a fraction of the distance between codes, keep moving.
  * sqrt(v) > 0 never becomes 0 (the smallest code instead); v itself is formed in fp32 and counts as 0 below 2^-126 (gradients of 1e-18 where beta2 is
- * 0.999). The step itself uses the moments before they are rounded.
+ * 0.999). The step itself uses the moments before they are rounded. Infinities and NaN are kept as NaN; the scale of their block is that of its
+ * finite magnitudes, so that the other elements keep theirs.
  */
 typedef struct {
   void* const* W;   /* [K][n] in w_dtype; on entry to lordo_adamw_init replica 0 holds the initial weights */

@@ -292,6 +292,19 @@ __device__ __forceinline__ unsigned low_positive(const float2 (&x)[4]) {
   return t;
 }
 
+// Bits of the largest finite magnitude of a lane's eight values. A scale is formed of these where a block holds an infinity or NaN: those are lost in
+// any case, and a scale that followed them (2^121) would take the block's other 255 moments along.
+constexpr unsigned kInfinity = 0x7F800000u;
+__device__ __forceinline__ unsigned top_finite(const float2 (&x)[4]) {
+  unsigned t = 0u;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const unsigned b = __float_as_uint(j & 1 ? x[j >> 1].y : x[j >> 1].x) & 0x7FFFFFFFu;
+    if (b < kInfinity && b > t) t = b;
+  }
+  return t;
+}
+
 // 16 x + y. Written out: as a shift by four, nvcc 12.9 lost it where x came from one half of a packed product and the result's top byte was taken.
 __device__ __forceinline__ unsigned mad16(unsigned x, unsigned y) {
   unsigned r;
@@ -400,7 +413,12 @@ __device__ __forceinline__ void step8_lane(const Step8& s, unsigned long long co
       v[at] = __ffma2_rn(__fmul2_rn(b2, __fmul2_rn(y[j], y[j])), one, __fmul2_rn(__fmul2_rn(a2, z), z));
     }
   }
-  const unsigned mtop = __reduce_max_sync(0xffffffffu, top_signed(m)), vtop = __reduce_max_sync(0xffffffffu, top_positive(v));
+  unsigned mtop = __reduce_max_sync(0xffffffffu, top_signed(m)), vtop = __reduce_max_sync(0xffffffffu, top_positive(v));
+  const bool lost = (mtop > vtop ? mtop : vtop) >= kInfinity;
+  if (lost) {
+    mtop = __reduce_max_sync(0xffffffffu, top_finite(m));
+    vtop = __reduce_max_sync(0xffffffffu, top_finite(v));
+  }
   const float rtop = root<false>(both(__uint_as_float(vtop))).x;
   mcode = scale_code(mtop);
   vcode = scale_code(__float_as_uint(rtop));
@@ -408,10 +426,10 @@ __device__ __forceinline__ void step8_lane(const Step8& s, unsigned long long co
   // scales above 2^6 (their reciprocal's 2^-120 would not be a normal number), infinities, NaN; v whose root is below the smallest code, or not normal
   constexpr unsigned kLarge = (127u + 14u) << 23;
   const float least = fmaxf(0x1p-18f * (pow2(vcode) * pow2(vcode)), 0x1p-126f);
-  const bool slow = mtop >= kLarge || __float_as_uint(rtop) >= kLarge || __any_sync(0xffffffffu, __uint_as_float(low_positive(v)) < least);
+  const bool slow = lost || mtop >= kLarge || __float_as_uint(rtop) >= kLarge || __any_sync(0xffffffffu, __uint_as_float(low_positive(v)) < least);
   if (!slow) {
     finish8<true, QHM>(s, counter, g, m, v, w, mc, vc, mi, vi);
-  } else if (mtop | vtop) {
+  } else if (lost || (mtop | vtop)) {
     finish8<false, QHM>(s, counter, g, m, v, w, mc, vc, mi, vi);
   } else {  // a block that never had a gradient
 #pragma unroll
@@ -790,7 +808,9 @@ __device__ __forceinline__ void outer_mean8(const AwTensor& T, int K, float inv_
     a[j] = __fmul2_rn(a[j], both(inv_k));
     if (SECOND) a[j] = root<false>(a[j]);
   }
-  const int code = scale_code(__reduce_max_sync(0xffffffffu, SECOND ? top_positive(a) : top_signed(a)));
+  unsigned top = __reduce_max_sync(0xffffffffu, SECOND ? top_positive(a) : top_signed(a));
+  if (top >= kInfinity) top = __reduce_max_sync(0xffffffffu, top_finite(a));
+  const int code = scale_code(top);
   const float inv = pow2(254 - code);
   unsigned c[2];
 #pragma unroll

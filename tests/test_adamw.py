@@ -570,3 +570,42 @@ def test_a_round_beside_the_low_rank_path(states):
     assert low.poll_status() == 0 and rest.poll_status() == 0 and rest.counters() == [2 * H, 2]
     assert (rest.storage["W"] != first).float().mean() > 0.5
     low.close(), rest.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan"), 1e25])
+@pytest.mark.parametrize("n", [300, 4096])
+@pytest.mark.parametrize("states", ["f32", "8bit"])
+def test_a_nonfinite_gradient_stays_in_its_elements(states, bad, n):
+    """Four steps and a synchronisation after one worker's infinity or NaN, in a block with others and in a block of nothing else: all other elements,
+    and all scales, have the bits of a group whose gradients are 0 there. (1e25: v is infinite, m is not, and is its block's largest, so that 8-bit
+    neighbours lose theirs: they stay finite.)"""
+    K, shapes = 3, [(n,), (77,)]
+    hit = torch.zeros(n, dtype=torch.bool, device="cuda")
+    hit[5] = True
+    hit[256:512] = n > 512
+    kw = dict(states=states, eps=1e-3, seed=6, outer=lordo.OUTER_NESTEROV, outer_lr=0.7, outer_momentum=0.9)
+    a, b = (group(shapes, K, 1, **kw) for _ in range(2))
+    coef = torch.ones(K, device="cuda")
+    for s in range(4):
+        G = gradients(shapes, K, s, "f32")
+        G[0][:, hit] = 0.0
+        b.step(G, 0.01, coef=coef)
+        if s == 0:
+            G[0][1, hit] = bad
+        a.step(G, 0.01, coef=coef)
+        if s == 2:
+            a.outer_step(), b.outer_step()
+        worker = slice(0, K) if s >= 2 else slice(1, 2)
+        bits = lambda x: x.view(torch.uint8 if x.element_size() == 1 else torch.int32)
+        for name in ("W", "m", "v", "ms", "vs"):
+            for i, (x, y) in enumerate(zip(getattr(a, name), getattr(b, name))):
+                rest = ~hit if name in ("W", "m", "v") and i == 0 else slice(None)
+                if abs(bad) < float("inf") and i == 0 and name not in ("v", "vs"):
+                    assert torch.isfinite(x.float()[:, rest]).all(), (s, name)
+                else:
+                    assert torch.equal(bits(x)[:, rest], bits(y)[:, rest]), (s, name, i)
+        assert not torch.isfinite(a.v[0][worker].float()[:, hit]).any()
+        if not abs(bad) < float("inf"):
+            assert torch.isnan(a.W[0][worker][:, hit]).all()
+    a.close(), b.close()
