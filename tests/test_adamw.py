@@ -609,3 +609,28 @@ def test_a_nonfinite_gradient_stays_in_its_elements(states, bad, n):
         if not abs(bad) < float("inf"):
             assert torch.isnan(a.W[0][worker][:, hit]).all()
     a.close(), b.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lr,wd", [(1e-3, 0.1), (1e-5, 0.1), (1e-6, 0.1), (2e-7, 0.1), (1e-6, 0.01)])
+@pytest.mark.parametrize("omega", [1.0, 0.9])
+@pytest.mark.parametrize("states", ["f32", "8bit"])
+def test_weight_decay_far_below_a_step_of_the_weights(states, omega, lr, wd):
+    """The change of an fp32 weight is formed apart and added once: off by half a step of the new weight, and by the roundings of the change itself.
+    Those, in half steps: the moments 4 and 6 (3 under the root), the constants 5 each, the products, the root (2), the quotient (2) and the
+    sums 8: at most 40 of the update, and 8 (the rates, their product, its product with the weight, the sum) of the decay. Blocks that never
+    had a gradient, a last block that is not whole, and workers at odd addresses."""
+    K = 2
+    for n in (256 * 40 + 100, 255 * 17):
+        gen = torch.Generator(device="cuda").manual_seed(n)
+        opt = adamw.AdamW([torch.randn(n, generator=gen, device="cuda")], K, states=states, eps=1e-3, weight_decay=wd, seed=2)
+        g = torch.randn(K, n, device="cuda", generator=gen)
+        g[:, 512:1024] = 0.0
+        W0 = ref.to64(opt.W[0])
+        opt.step([g], lr, 0.9, omega)
+        W, _, _, up = ref.adamw(W0, 0.0, 0.0, ref.to64(g), lr, 0.9, 0.999, omega, 1e-3, wd, 1)
+        got = ref.to64(opt.W[0])
+        step = np.spacing(np.maximum(np.abs(got), np.abs(W)).astype(np.float32)).astype(np.float64)
+        off = HALF["f32"] * (40 * lr * np.abs(up) + 8 * lr * wd * np.abs(W0))
+        assert (np.abs(got - W) <= step / 2 + off).all(), (np.abs(got - W) / step).max()
+        opt.close()
