@@ -16,7 +16,7 @@ from typing import Dict, List, NamedTuple, Optional, Sequence, Union
 import torch
 
 from . import lordo
-from .lordo import LordoError, _AdamWBuffers, _AdamWConfig, _Grad, _Tensor, _dtype_code, _ptr_table, load_library
+from .lordo import LordoError, _AdamWBuffers, _AdamWConfig, _Grad, _Tensor, _dtype_code, _ptr_table, load_library, used_on
 
 _INDEX = {torch.int32: 0, torch.int64: 1}
 _STATES = {"f32": 0, "8bit": 1}
@@ -120,7 +120,6 @@ class AdamW:
         self._grad_at, self._tokens_at = words[0::4], words[1::4]
         self._no_tokens = memoryview(array("Q", bytes(8 * len(n))))
         self._full = [torch.Size((self.K,) + s) for s in self.shapes]
-        self._keep = None
 
     # -- helpers -----------------------------------------------------------------------------
     def _check(self, rc: int, where: str):
@@ -151,7 +150,8 @@ class AdamW:
     def step(self, G: Sequence[Union[torch.Tensor, TokenGrad]], lr: float, beta1: float = 0.9, omega: float = 1.0,
              coef: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
         """One step. G: per tensor [K, *shape] in g_dtype, or TokenGrad. coef: K clip coefficients in device memory in place of the
-        group's own (for instance those of a Lordo)."""
+        group's own (for instance those of a Lordo). All may be dropped after the call: with ``stream`` they are recorded on it. Its order with the
+        streams that make them is the caller's."""
         if len(G) != len(self.shapes):
             raise ValueError(f"{len(self.shapes)} gradients are wanted, not {len(G)}")
         dt, index, at = self.g_dtype, self.device.index, array("Q")
@@ -166,9 +166,12 @@ class AdamW:
         self._grad_at[:] = memoryview(at)
         if coef is not None and (coef.dtype != torch.float32 or coef.numel() != self.K or coef.device != self.device or not coef.is_contiguous()):
             raise ValueError(f"coef: {self.K} contiguous float32 values on {self.device} are wanted")
-        self._keep = (list(G), coef)  # alive until the next step: `stream` need not be the one they were allocated on
-        self._check(self._run(self.lib.lordo_adamw_step, self._grads, lr, beta1, omega, coef.data_ptr() if coef is not None else None, self._stream(stream)),
-                    "lordo_adamw_step")
+        rc = self._run(self.lib.lordo_adamw_step, self._grads, lr, beta1, omega, coef.data_ptr() if coef is not None else None, self._stream(stream))
+        if stream is not None:
+            for g in G:
+                used_on(stream, *(g[:2] if g.__class__ is TokenGrad else (g,)))
+            used_on(stream, coef)
+        self._check(rc, "lordo_adamw_step")
 
     def _run(self, call, *args) -> int:
         """A call that launches, with the group's device current."""

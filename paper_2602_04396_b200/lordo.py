@@ -162,6 +162,13 @@ def _stream_handle(stream: Optional[torch.cuda.Stream]) -> C.c_void_p:
     return C.c_void_p(s.cuda_stream)
 
 
+def used_on(stream: torch.cuda.Stream, *tensors: Optional[torch.Tensor]) -> None:
+    """Tells the allocator that `stream` works on the tensors: memory that the caller drops is handed out again only when the stream is past this point."""
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+
+
 def make_config(mats: Sequence[Tuple[int, int, int]], K: int, H: int, *, w_dtype=F32, g_dtype=F32, e_dtype=F32,
                 variant=GLOBAL, error_feedback=True, beta2=0.999, eps=1e-8, clip_rho=0.0, clip_scope=0, sync_u=True,
                 sync_v=True, outer=OUTER_AVG, outer_lr=1.0, outer_momentum=0.0, power_iters=0, seed=0, check_mode=1, warm_start=0, time_buffer=0, oversample=0,

@@ -634,3 +634,55 @@ def test_weight_decay_far_below_a_step_of_the_weights(states, omega, lr, wd):
         off = HALF["f32"] * (40 * lr * np.abs(up) + 8 * lr * wd * np.abs(W0))
         assert (np.abs(got - W) <= step / 2 + off).all(), (np.abs(got - W) / step).max()
         opt.close()
+
+
+def _junk_like(tensors):
+    """Takes memory of the same sizes and fills it: with what allocations of the current stream that were given back have left."""
+    return [torch.full_like(t, -1 if t.dtype in (torch.int32, torch.int64) else float("nan")) for t in tensors]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("states", ["f32", "8bit"])
+def test_gradients_given_back_before_their_stream_has_come_to_them(states):
+    """Steps on a stream that is still busy with earlier work (a tenth of a second), gradients, tokens and coefficients allocated anew for each and
+    dropped at once, their memory taken and overwritten on the current stream: the bits of steps whose gradients were kept."""
+    K, shapes = 2, [(300, 512), (70000,)]
+    a, b = (group(shapes, K, 1, states=states, tables={0: 64}, seed=3) for _ in range(2))
+
+    def make(s):
+        gen = torch.Generator(device="cuda").manual_seed(s)
+        tok = torch.randint(0, 300, (K, 64), device="cuda", generator=gen)
+        dY = torch.randn(K, 64, 512, device="cuda", generator=gen)
+        return tok, dY, torch.randn(K, 70000, device="cuda", generator=gen), torch.rand(K, device="cuda", generator=gen)
+
+    kept = [make(s) for s in range(6)]
+    for tok, dY, g, coef in kept:
+        b.step([adamw.TokenGrad(tok, dY), g], 0.01, coef=coef)
+    side, junk = torch.cuda.Stream(), [_junk_like(kept[0])]  # its kernels are loaded by now
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+    for s in range(6):
+        tok, dY, g, coef = make(s)
+        torch.cuda.current_stream().synchronize()
+        a.step([adamw.TokenGrad(tok, dY), g], 0.01, coef=coef, stream=side)
+        del tok, dY, g, coef
+        junk.append(_junk_like(kept[s]))
+    torch.cuda.synchronize()
+    for x in a.storage:
+        assert torch.equal(a.storage[x].view(torch.uint8), b.storage[x].view(torch.uint8)), x
+    a.close(), b.close()
+
+
+@pytest.mark.gpu
+def test_gradients_are_not_held_after_the_step():
+    """On the current stream the allocator's own order is enough: a step keeps nothing that its caller has dropped."""
+    import weakref
+    opt = group([(50, 8), (9,)], 2, 1, tables={0: 4})
+    tok, dY, g = torch.zeros(2, 4, device="cuda", dtype=torch.int64), torch.ones(2, 4, 8, device="cuda"), torch.ones(2, 9, device="cuda")
+    coef = torch.ones(2, device="cuda")
+    held = [weakref.ref(x) for x in (tok, dY, g, coef)]
+    opt.step([adamw.TokenGrad(tok, dY), g], 0.01, coef=coef)
+    del tok, dY, g, coef
+    assert all(r() is None for r in held)
+    opt.close()
