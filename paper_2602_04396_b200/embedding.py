@@ -2,7 +2,8 @@
 
 For one table, or for the K workers' replicas of one: ``W`` is [V, d] with tokens of any shape, or [K, V, d] with tokens [K, ...].
 Tokens are int32 or int64; one outside [0, V) is padding: a row of zeros, and no share in the gradient. Both calls work on
-the tensors' device, enqueue on ``stream`` (default: the device's current one) and can be captured in a CUDA graph.
+the tensors' device, enqueue on ``stream`` (default: the device's current one) and can be captured in a CUDA graph. What a call allocates
+belongs to its stream; with ``stream`` the tensors handed over are recorded on it, so that they may be dropped after the call.
 """
 from __future__ import annotations
 
@@ -12,7 +13,7 @@ from typing import Optional
 
 import torch
 
-from .lordo import LordoError, _dtype_code, load_library
+from .lordo import LordoError, _dtype_code, load_library, used_on
 
 _INDEX = {torch.int32: 0, torch.int64: 1}
 _raw_stream = torch._C._cuda_getCurrentRawStream  # torch.cuda.current_stream builds an object: 3 us of a call's 10
@@ -56,7 +57,10 @@ def embedding(W: torch.Tensor, tokens: torch.Tensor, *, scale: float = 1.0, out:
     context = _on(device, stream) if device >= 0 else None
     if context is not None:
         with context:
-            return embedding(W, tokens, scale=scale, out=out, out_dtype=out_dtype)
+            result = embedding(W, tokens, scale=scale, out=out, out_dtype=out_dtype)
+        if stream is not None:
+            used_on(stream, W, tokens, out)
+        return result
     _checked(W, "W", device)
     _checked(tokens, "tokens", device)
     if W.dim() not in (2, 3):
@@ -89,7 +93,10 @@ def embedding_grad(dY: torch.Tensor, tokens: torch.Tensor, V: int, *, scale: flo
     context = _on(device, stream) if device >= 0 else None
     if context is not None:
         with context:
-            return embedding_grad(dY, tokens, V, scale=scale, out=out, out_dtype=out_dtype, accumulate=accumulate, K=K)
+            result = embedding_grad(dY, tokens, V, scale=scale, out=out, out_dtype=out_dtype, accumulate=accumulate, K=K)
+        if stream is not None:
+            used_on(stream, dY, tokens, out)
+        return result
     _checked(dY, "dY", device)
     _checked(tokens, "tokens", device)
     d = dY.shape[-1]

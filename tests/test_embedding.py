@@ -251,3 +251,37 @@ def test_binding_refusals():
             call()
     with pytest.raises(lordo.LordoError):
         embedding.embedding_grad(dY, tok, 0, K=2)
+
+
+@pytest.mark.gpu
+def test_inputs_given_back_before_their_stream_has_come_to_them():
+    """Calls on a stream that is still busy with earlier work (a tenth of a second), their inputs dropped at once and their memory taken and
+    overwritten on the current stream: the bits of calls whose inputs were kept."""
+    K, V, d, T = 2, 900, 256, 700
+
+    def make(s):
+        gen = torch.Generator(device="cuda").manual_seed(s)
+        return (torch.randn(K, V, d, device="cuda", generator=gen), torch.randint(-1, V, (K, T), device="cuda", generator=gen),
+                torch.randn(K, T, d, device="cuda", generator=gen), torch.randint(-1, V, (K, T), device="cuda", generator=gen, dtype=torch.int32))
+
+    kept = [make(s) for s in range(4)]
+    want = [(embedding.embedding(W, t), embedding.embedding_grad(dY, u, V, K=K)) for W, t, dY, u in kept]
+    added = [embedding.embedding_grad(dY, u, V, out=W.clone(), accumulate=True) for W, _, dY, u in kept]
+    side, got, junk = torch.cuda.Stream(), [], [[torch.full_like(x, -1) for x in kept[0]]]  # its kernels are loaded by now
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+    for s in range(4):
+        W, t, dY, u = make(s)
+        torch.cuda.current_stream().synchronize()
+        first = embedding.embedding(W, t, stream=side), embedding.embedding_grad(dY, u, V, K=K, stream=side)
+        del t
+        got.append(first)
+        with torch.cuda.stream(side):  # a copy that is made where the table is still whole
+            embedding.embedding_grad(dY, u, V, out=W, accumulate=True, stream=side)
+            got[-1] += (W.clone(),)
+        del W, dY, u
+        junk.append([torch.full_like(x, -1 if x.dtype in (torch.int32, torch.int64) else float("nan")) for x in kept[s]])
+    torch.cuda.synchronize()
+    for g, w, a in zip(got, want, added):
+        assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1]) and torch.equal(g[2], a)
