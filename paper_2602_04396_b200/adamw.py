@@ -127,7 +127,11 @@ class AdamW:
             raise LordoError(rc, where, self.lib.lordo_adamw_last_error(self._ctx).decode())
 
     def _stream(self, stream: Optional[torch.cuda.Stream]) -> int:
-        return stream.cuda_stream if stream is not None else _raw_stream(self.device.index)
+        if stream is None:
+            return _raw_stream(self.device.index)
+        if stream.device != self.device:
+            raise ValueError(f"stream: one of {self.device} is wanted, not of {stream.device}")
+        return stream.cuda_stream
 
     def _token_grad(self, i: int, g: TokenGrad) -> int:
         """Fills the gradient's entry but for the address of dY, which is returned."""

@@ -36,6 +36,8 @@ def _tokens_per_worker(tokens: torch.Tensor, K: int, table: bool) -> int:
 def _on(index: int, stream: Optional[torch.cuda.Stream]):
     """A context with the device current, and `stream` too where one is given, so that what is allocated belongs to it; None where it is so already."""
     if stream is not None:
+        if stream.device.index != index:
+            raise ValueError(f"stream: one of device {index} is wanted, not of {stream.device}")
         return torch.cuda.stream(stream)
     return None if index == torch.cuda.current_device() else torch.cuda.device(index)
 

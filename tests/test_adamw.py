@@ -686,3 +686,18 @@ def test_gradients_are_not_held_after_the_step():
     del tok, dY, g, coef
     assert all(r() is None for r in held)
     opt.close()
+
+
+@pytest.mark.gpu
+def test_a_stream_of_another_device():
+    class Other:
+        device, cuda_stream = torch.device("cuda", 1), 0
+
+    opt = adamw.AdamW([torch.ones(9)], 2, device="cuda:0", outer=lordo.OUTER_AVG)
+    g = torch.ones(2, 9, device="cuda:0")
+    for call in (lambda: opt.step([g], 0.1, stream=Other()), lambda: opt.outer_step(stream=Other()), lambda: opt.poll_status(stream=Other()),
+                 lambda: opt.clear_status(stream=Other())):
+        with pytest.raises(ValueError, match="stream"):
+            call()
+    assert opt.counters() == [0, 0] and (opt.W[0] == 1).all()
+    opt.close()

@@ -285,3 +285,16 @@ def test_inputs_given_back_before_their_stream_has_come_to_them():
     torch.cuda.synchronize()
     for g, w, a in zip(got, want, added):
         assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1]) and torch.equal(g[2], a)
+
+
+@pytest.mark.gpu
+def test_a_stream_of_another_device():
+    """Refused, not replaced by the current stream of the tensors' device."""
+    class Other:
+        device, cuda_stream = torch.device("cuda", 1), 0
+
+    W, tok = torch.zeros(9, 8, device="cuda:0"), torch.tensor([1, 3], device="cuda:0")
+    with pytest.raises(ValueError, match="stream"):
+        embedding.embedding(W, tok, stream=Other())
+    with pytest.raises(ValueError, match="stream"):
+        embedding.embedding_grad(torch.zeros(2, 8, device="cuda:0"), tok, 9, stream=Other())
