@@ -404,8 +404,9 @@ LORDO_API int lordo_adamw_init(const lordo_adamw_config* cfg, const lordo_adamw_
  *   W <- W - lr ((omega m^ + (1-omega) g) / (sqrt(v^) + eps) + weight_decay W)
  * omega = 1 is AdamW, omega < 1 the quasi-hyperbolic form of the low-rank path. c_k = min(1, rho / (norm + 1e-6)), or, with coef_dev
  * (K floats in device memory), coef_dev[k]: for instance the coefficients of a lordo_ctx. s counts the steps of this context. A gradient
- * norm that is NaN or infinite sets LORDO_FLAG_NONFINITE_GRAD (only where the norm is formed). The step count and the rates are host
- * values, so a stream that is being captured is refused (LORDO_ERR_UNSUPPORTED).
+ * norm that is NaN or infinite sets LORDO_FLAG_NONFINITE_GRAD (only where the norm is formed); its coefficient is then NaN or 0,
+ * as the formula has it (lordo_inner_step takes 1 for NaN). The step count and the rates are host values, so a stream that is being
+ * captured is refused (LORDO_ERR_UNSUPPORTED).
  */
 LORDO_API int lordo_adamw_step(lordo_adamw_ctx* ctx, const lordo_grad* G, double lr, double beta1, double omega, const float* coef_dev,
                                void* stream);

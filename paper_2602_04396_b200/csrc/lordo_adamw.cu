@@ -165,7 +165,8 @@ __global__ void __launch_bounds__(256) adamw_norm_kernel(const __grid_constant__
   for (unsigned x = t; x < many; x += 256) a += __ldcg(p + x);
   const double total = block_sum(a, red[1]);
   if (t == 0 && !isfinite(total)) atomicOr(c.status, LORDO_FLAG_NONFINITE_GRAD);
-  const float coef = (float)fmin(1.0, c.rho / (sqrt(total) + 1e-6));
+  const double ratio = c.rho / (sqrt(total) + 1e-6);
+  const float coef = ratio >= 1.0 ? 1.f : (float)ratio;  // NaN stays what it is: fmin's 1 would leave the rest of a gradient that holds one unclipped
   if (c.scope) {
     if (t == 0) c.coef[(long long)index * l.K + k] = coef;
   } else {

@@ -701,3 +701,28 @@ def test_a_stream_of_another_device():
             call()
     assert opt.counters() == [0, 0] and (opt.W[0] == 1).all()
     opt.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scope", [0, 1])
+@pytest.mark.parametrize("tokens", [False, True])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_clip_coefficient_of_a_nan(scope, tokens, dt):
+    """min(1, rho / (norm + 1e-6)) of a NaN is NaN, not 1: a NaN does not turn clipping off for the rest of its norm. Of an infinity it is 0."""
+    K, shapes = 3, [(40, 24), (300,), (5,)]
+    for bad, want in ((float("nan"), float("nan")), (float("inf"), 0.0)):
+        opt = group(shapes, K, 1, g_dtype=DT[dt], clip_rho=1.0, clip_scope=scope, tables={0: 30} if tokens else None)
+        G = gradients(shapes, K, 1, dt)
+        tok = torch.arange(30, device="cuda").repeat(K, 1)
+        dY = gradients([(30, 24)], K, 2, dt)[0]
+        G64 = [ref.table_grad(tok.cpu().numpy(), ref.to64(dY), 40, 1.0).reshape(K, -1) if tokens else ref.to64(G[0]).reshape(K, -1), ref.to64(G[1]), ref.to64(G[2])]
+        coef = ref.clip(G64, 1.0, scope)
+        (dY if tokens else G[0])[1, 7, 3] = bad
+        opt.step([adamw.TokenGrad(tok, dY) if tokens else G[0]] + G[1:], 0.01)
+        got = ref.to64(opt.clip_coefficients())
+        hit = np.zeros((3, K), bool)
+        hit[slice(0, 3) if scope == 0 else 0, 1] = True
+        assert np.array_equal(got[hit], np.full(hit.sum(), want), equal_nan=True)
+        assert (np.abs(got - coef)[~hit] <= COEF * coef[~hit]).all()
+        assert opt.poll_status() == lordo.FLAG_NONFINITE_GRAD
+        opt.close()
