@@ -138,6 +138,15 @@ __global__ void __launch_bounds__(256) adamw_norm_kernel(const __grid_constant__
       }
     }
     s = part[0] + part[1];
+    if (!(s < INFINITY)) {  // fp32 does not hold the squares of gradients above 6e18: the thread's once more, all in fp64
+      s = 0.0;
+      for (long long f = a0 + 8 * t; f < a1; f += 2048) {
+        float g[8];
+        load8<GDT>(G, f, g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += (double)g[j] * (double)g[j];
+      }
+    }
     const long long edge = t < 8 ? f0 + t : (a1 > a0 ? a1 : a0) + t - 8;  // elements before the first and behind the last vector
     if (t < 16 && edge < f1 && (t >= 8 || edge < a0)) {
       const float x = load1(G, GDT, edge);

@@ -383,15 +383,22 @@ struct Old {
   }
 };
 
-// The sum of token v, whose first sorted entry is `start`; old: the row it is added to.
+// The sum of token v, whose first sorted entry is `start`; old: the row it is added to; sq: squares of a row's VEC columns in fp32, of rows in fp64.
 template <int VEC, int MODE, int ODT>
-__device__ __forceinline__ void emit(const SumArgs& a, int k, int v, int start, long long col, float (&acc)[VEC], const Old<ODT, VEC>& old, float& sq) {
+__device__ __forceinline__ void emit(const SumArgs& a, int k, int v, int start, long long col, float (&acc)[VEC], const Old<ODT, VEC>& old, double& sq) {
 #pragma unroll
   for (int j = 0; j < VEC; ++j) acc[j] *= a.scale;
   if (MODE == SUM_ROWS) {
     put<VEC>(a.out, LORDO_F32, ((long long)k * a.out_cap + start) * a.d + col, acc);
+    float squares = 0.f;
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) sq += acc[j] * acc[j];
+    for (int j = 0; j < VEC; ++j) squares += acc[j] * acc[j];
+    if (squares < INFINITY) {
+      sq += (double)squares;
+    } else {  // fp32 does not hold them, though it may each sum
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) sq += (double)acc[j] * (double)acc[j];
+    }
   } else {
     if (MODE == SUM_ADD) {
 #pragma unroll
@@ -402,9 +409,8 @@ __device__ __forceinline__ void emit(const SumArgs& a, int k, int v, int start, 
 }
 
 // Sums of squares of a block: sq[k][which * gridDim.x + block].
-__device__ __forceinline__ void block_squares(const SumArgs& a, int k, int which, float x) {
+__device__ __forceinline__ void block_squares(const SumArgs& a, int k, int which, double s) {
   __shared__ double red[8];
-  double s = (double)x;
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
   __syncthreads();
@@ -420,7 +426,7 @@ __device__ __forceinline__ void block_squares(const SumArgs& a, int k, int which
 // the window are done; the first part of one that goes on and the last of one that came in are left for join_sums_kernel.
 constexpr int kAhead = 8;
 template <int DT, int VEC, int MODE, int W, int ODT>
-__device__ __forceinline__ void window_sums(const SumArgs& a, int k, int w, long long col, int lane, float& sq) {
+__device__ __forceinline__ void window_sums(const SumArgs& a, int k, int w, long long col, int lane, double& sq) {
   const int valid = a.valid[k], s = w * W;
   if (s >= valid) return;
   const int n = valid - s < W ? valid - s : W;
@@ -501,7 +507,7 @@ __global__ void __launch_bounds__(256) window_sums_kernel(SumArgs a) {
   }
   const long long item = (long long)blockIdx.x * 8 + warp;
   const long long w = item / a.groups;
-  float sq = 0.f;
+  double sq = 0.0;
   if (w < a.windows) window_sums<DT, VEC, MODE, W, ODT>(a, k, (int)w, ((item - w * a.groups) * 32 + lane) * VEC, lane, sq);
   if (MODE == SUM_ROWS) block_squares(a, k, 0, sq);
 }
@@ -519,7 +525,7 @@ __global__ void __launch_bounds__(256) join_sums_kernel(SumArgs a) {
   const int w = (int)(item / a.groups);
   const long long col = ((item - (long long)w * a.groups) * 32 + lane) * VEC;
   const int valid = a.valid[k], last = (w + 1) * W - 1;
-  float sq = 0.f;
+  double sq = 0.0;
   if (w < a.windows && last + 1 < valid) {
     const int2* order = a.order + (long long)k * a.T;
     const int v = __ldcg(order + last).x;

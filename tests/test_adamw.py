@@ -726,3 +726,37 @@ def test_clip_coefficient_of_a_nan(scope, tokens, dt):
         assert (np.abs(got - coef)[~hit] <= COEF * coef[~hit]).all()
         assert opt.poll_status() == lordo.FLAG_NONFINITE_GRAD
         opt.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [6e18, 1e20, 1e36])
+@pytest.mark.parametrize("tokens", [False, True])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_norm_of_gradients_whose_squares_pass_fp32(size, tokens, dt):
+    """The sum of squares of a finite gradient is a finite fp64 number: its coefficient is the definition's, and no flag is set. Tokens are all
+    different and the scale is 1, so that a row's sum is the row."""
+    K, V, d = 2, 2100, 40
+    shapes = [(V, d), (9,)]
+    opt = group(shapes, K, 1, g_dtype=DT[dt], clip_rho=0.5, tables={0: V} if tokens else None)
+    G = gradients(shapes, K, 1, dt, std=1.0)
+    G[0] = (G[0].float() * size / G[0].float().abs().max()).to(DT[dt])
+    coef = ref.clip([ref.to64(x).reshape(K, -1) for x in G], 0.5)
+    opt.step([adamw.TokenGrad(torch.arange(V, device="cuda").repeat(K, 1), G[0]) if tokens else G[0], G[1]], 0.01)
+    assert (np.abs(ref.to64(opt.clip_coefficients()) - coef) <= COEF * coef).all()
+    assert opt.poll_status() == 0 and torch.isfinite(opt.W[0]).all()
+    opt.close()
+
+
+@pytest.mark.gpu
+def test_squares_of_rows_summed_by_token_are_widened_row_by_row():
+    """Sums of squares of a table's rows, 32 rows of a window one after another: one row of size 1 (its columns' squares are exact in any order), then
+    31 whose squares are 2^-26 each. Added to the first in fp32, each of them would be lost; here they are 31 2^-26 of the norm's square,
+    of which a coefficient with a rounding of 2^-24 and a root keeps all but 2^-23."""
+    V, d = 32, 8
+    opt = adamw.AdamW([torch.zeros(V, d)], 1, clip_rho=1e-3, tables={0: V})
+    dY = torch.full((1, V, d), 2.0 ** -13, device="cuda")
+    dY[0, 0] = 1.0
+    opt.step([adamw.TokenGrad(torch.arange(V, device="cuda").view(1, V), dY)], 0.0)
+    norm = (8 * (1 + 31 * 2.0 ** -26)) ** 0.5
+    assert abs(float(opt.clip_coefficients()[0, 0].double()) / (1e-3 / (norm + 1e-6)) - 1) <= 2.0 ** -23
+    opt.close()
