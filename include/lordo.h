@@ -349,7 +349,7 @@ typedef struct {
   int32_t K;                   /* workers held as replicas, 1 .. 64 */
   int32_t w_dtype, g_dtype;    /* lordo_dtype */
   int32_t states;              /* lordo_states: the moments in fp32, or in 8 bits (below) */
-  double beta2, eps;           /* eps > 0. Rates are doubles here: 1 - 0.999f is 1.3e-5 off 0.001 */
+  double beta2, eps;           /* eps > 0; with 8-bit moments at least 2^-126. Rates are doubles here: 1 - 0.999f is 1.3e-5 off 0.001 */
   double clip_rho;             /* clipping radius; <= 0 disables clipping */
   int32_t clip_scope;          /* 0: one norm per worker over all tensors; 1: one per tensor */
   int32_t sync;                /* 1: the group takes part in synchronisations (X0, B); 0: lordo_adamw_outer_step is refused */

@@ -1,4 +1,5 @@
 // Host layer of the AdamW groups: context, workspace carving, the C ABI.
+#include <cfloat>
 #include <cmath>
 #include <new>
 #include <string>
@@ -64,6 +65,8 @@ int validate(const lordo_adamw_config* cfg) {
   if (!dt_ok(cfg->w_dtype) || !dt_ok(cfg->g_dtype)) return LORDO_ERR_INVALID_ARG;
   if (cfg->states != LORDO_STATES_F32 && cfg->states != LORDO_STATES_8BIT) return LORDO_ERR_INVALID_ARG;
   if (!(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) || !((float)cfg->eps > 0.f)) return LORDO_ERR_INVALID_ARG;
+  // the reciprocal of the 8-bit step takes a subnormal denominator for 0: an element without a gradient would be 0 times infinity
+  if (cfg->states == LORDO_STATES_8BIT && (float)cfg->eps < FLT_MIN) return LORDO_ERR_INVALID_ARG;
   if (cfg->clip_scope != 0 && cfg->clip_scope != 1) return LORDO_ERR_INVALID_ARG;
   if (cfg->outer != LORDO_OUTER_AVG && cfg->outer != LORDO_OUTER_NESTEROV) return LORDO_ERR_INVALID_ARG;
   long long elements = 0;

@@ -760,3 +760,28 @@ def test_squares_of_rows_summed_by_token_are_widened_row_by_row():
     norm = (8 * (1 + 31 * 2.0 ** -26)) ** 0.5
     assert abs(float(opt.clip_coefficients()[0, 0].double()) / (1e-3 / (norm + 1e-6)) - 1) <= 2.0 ** -23
     opt.close()
+
+
+def test_eps_below_the_normal_numbers(lib):
+    """In 8 bits the quotient is taken by a reciprocal that takes subnormal numbers for 0: an element without a gradient would be 0 times infinity."""
+    tensors = (lordo._Tensor * 1)(lordo._Tensor(100, 0, 0, 0.0))
+
+    def query(states, eps):
+        cfg = lordo._AdamWConfig(1, tensors, 2, 0, 0, states, 0.999, eps, 0.0, 0, 0, 0, 0, 0, 1.0, 0.0, 0)
+        out = C.c_size_t(0)
+        return lib.lordo_adamw_query_workspace(C.byref(cfg), C.byref(out))
+
+    assert query(1, 1e-39) == 1 and query(1, 2.0 ** -127) == 1 and query(1, 2.0 ** -126) == 0 and query(1, 1e-8) == 0
+    assert query(0, 1e-39) == 0 and query(0, 1e-50) == 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("states,eps", [("f32", 1e-39), ("f32", 2.0 ** -126), ("8bit", 2.0 ** -126)])
+def test_elements_without_a_gradient_at_the_least_eps(states, eps):
+    opt = adamw.AdamW([torch.ones(600)], 1, states=states, eps=eps)
+    g = torch.zeros(1, 600, device="cuda")
+    g[0, ::7] = 1.0
+    opt.step([g], 0.5)
+    assert (opt.W[0][g == 0] == 1.0).all()
+    assert ((opt.W[0][g != 0] - 0.5).abs() <= 0.5 * 40 * HALF["f32"]).all()  # half of an update of 1, see above
+    opt.close()
