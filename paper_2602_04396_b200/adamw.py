@@ -105,7 +105,7 @@ class AdamW:
                     views[name].append(flat[o:o + s].view(((self.K,) if replicas else ()) + shape))
             self.W, self.m, self.v, self.ms, self.vs, self.X0, self.B = (views[x] for x in ("W", "m", "v", "ms", "vs", "X0", "B"))
             for w, w0 in zip(self.W, W0):
-                w[0].copy_(w0)
+                w[0].copy_(w0.detach())  # a parameter would make the arrays part of its graph
             self._pointers = {name: _ptr_table(v, len(n)) for name, v in views.items() if v}
             bufs = _AdamWBuffers(*[C.cast(self._pointers[x], C.POINTER(C.c_void_p)) if x in self._pointers else None
                                    for x in ("W", "m", "v", "ms", "vs", "X0", "B")])

@@ -238,7 +238,7 @@ class Lordo:
         self.W, self.E, self.P, self.u, self.v, self.X0, self.B, self.Delta = [], [], [], [], [], [], [], []
         for (m, n, r), w0, side in zip(self.mats, W0, self.sides):
             w = z((K, m, n), w_dt)
-            w[0].copy_(w0.to(dev))
+            w[0].copy_(w0.detach().to(dev))  # a parameter would make the array part of its graph
             self.W.append(w)
             self.E.append(z((K, m, n), e_dtype) if self.error_feedback else None)
             pm, ln = (n, m) if side else (m, n)  # rows of the basis, columns of the low-rank moments

@@ -785,3 +785,15 @@ def test_elements_without_a_gradient_at_the_least_eps(states, eps):
     assert (opt.W[0][g == 0] == 1.0).all()
     assert ((opt.W[0][g != 0] - 0.5).abs() <= 0.5 * 40 * HALF["f32"]).all()  # half of an update of 1, see above
     opt.close()
+
+
+@pytest.mark.gpu
+def test_parameters_as_initial_weights():
+    """W0 may be a module's parameters: the group's arrays are no part of their graph."""
+    first = torch.nn.Parameter(torch.randn(6, 4))
+    opt = adamw.AdamW([first], 2, outer=lordo.OUTER_AVG)
+    low = lordo.Lordo([(32, 32, 8)], 2, 1, [torch.nn.Parameter(torch.randn(32, 32))])
+    assert torch.equal(opt.W[0][1].cpu(), first.detach())
+    for x in list(opt.storage.values()) + opt.W + low.W:
+        assert not x.requires_grad and x.grad_fn is None
+    opt.close(), low.close()
