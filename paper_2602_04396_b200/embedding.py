@@ -54,7 +54,8 @@ def _workspace(K: int, V: int, d: int, T: int) -> int:
 
 def embedding(W: torch.Tensor, tokens: torch.Tensor, *, scale: float = 1.0, out: Optional[torch.Tensor] = None,
               out_dtype: Optional[torch.dtype] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-    """scale * W[token], of shape tokens.shape + (d,) and of W's dtype unless ``out`` or ``out_dtype`` says otherwise."""
+    """scale * W[token], of shape tokens.shape + (d,) and of W's dtype unless ``out`` or ``out_dtype`` says otherwise. No part of autograd: a
+    table that requires a gradient is refused where one would be recorded (W.detach(), or a torch.autograd.Function around both calls)."""
     device = W.get_device()
     context = _on(device, stream) if device >= 0 else None
     if context is not None:
@@ -65,6 +66,8 @@ def embedding(W: torch.Tensor, tokens: torch.Tensor, *, scale: float = 1.0, out:
         return result
     _checked(W, "W", device)
     _checked(tokens, "tokens", device)
+    if W.requires_grad and torch.is_grad_enabled():
+        raise ValueError("W requires a gradient, which the lookup does not record: W.detach() and embedding_grad are wanted")
     if W.dim() not in (2, 3):
         raise ValueError("W: [V, d] or [K, V, d] is wanted")
     V, d = W.shape[-2:]

@@ -298,3 +298,15 @@ def test_a_stream_of_another_device():
         embedding.embedding(W, tok, stream=Other())
     with pytest.raises(ValueError, match="stream"):
         embedding.embedding_grad(torch.zeros(2, 8, device="cuda:0"), tok, 9, stream=Other())
+
+
+@pytest.mark.gpu
+def test_a_table_that_requires_a_gradient():
+    """The lookup is no part of autograd: where a gradient would be lost in silence the call is refused."""
+    W, tok = torch.randn(9, 8, device="cuda", requires_grad=True), torch.tensor([1, 3], device="cuda")
+    with pytest.raises(ValueError, match="detach"):
+        embedding.embedding(W, tok)
+    want = W.detach()[tok]
+    assert torch.equal(embedding.embedding(W.detach(), tok), want)
+    with torch.no_grad():
+        assert torch.equal(embedding.embedding(W, tok), want)
