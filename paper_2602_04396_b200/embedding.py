@@ -30,6 +30,8 @@ def _tokens_per_worker(tokens: torch.Tensor, K: int, table: bool) -> int:
         raise ValueError(f"tokens: int32 or int64 is wanted, not {tokens.dtype}")
     if table and (tokens.dim() < 2 or tokens.shape[0] != K):
         raise ValueError(f"tokens: [K, ...] with K = {K} is wanted, not {tuple(tokens.shape)}")
+    if K < 1:
+        raise ValueError("at least one worker is wanted")
     return tokens.numel() // K
 
 

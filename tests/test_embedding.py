@@ -310,3 +310,14 @@ def test_a_table_that_requires_a_gradient():
     assert torch.equal(embedding.embedding(W.detach(), tok), want)
     with torch.no_grad():
         assert torch.equal(embedding.embedding(W, tok), want)
+
+
+@pytest.mark.gpu
+def test_no_workers():
+    tok = torch.zeros(0, 3, device="cuda", dtype=torch.int64)
+    with pytest.raises(ValueError, match="worker"):
+        embedding.embedding(torch.zeros(0, 9, 8, device="cuda"), tok)
+    with pytest.raises(ValueError, match="worker"):
+        embedding.embedding_grad(torch.zeros(0, 3, 8, device="cuda"), tok, 9, K=0)
+    with pytest.raises(ValueError, match="worker"):
+        embedding.embedding_grad(torch.zeros(0, 3, 8, device="cuda"), tok, 9, out=torch.zeros(0, 9, 8, device="cuda"))
