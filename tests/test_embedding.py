@@ -321,3 +321,39 @@ def test_no_workers():
         embedding.embedding_grad(torch.zeros(0, 3, 8, device="cuda"), tok, 9, K=0)
     with pytest.raises(ValueError, match="worker"):
         embedding.embedding_grad(torch.zeros(0, 3, 8, device="cuda"), tok, 9, out=torch.zeros(0, 9, 8, device="cuda"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("K,V,d,T", SHAPES)
+@pytest.mark.parametrize("kind", ["uniform", "one", "pads", "few", "descending"])
+def test_gradient_from_fp32_into_bf16(K, V, d, T, kind):
+    """As test_gradient, four columns a lane and two bytes each in the table."""
+    test_gradient(K, V, d, T, "f32", "bf16", kind)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("K,V,d", [(2, 30000, 1000), (2, 90000, 333), (3, 30000, 768), (3, 130001, 96)])
+@pytest.mark.parametrize("dt,odt", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16")])
+def test_rows_without_a_token_of_a_large_table(K, V, d, dt, odt):
+    """Tables above 100 MB, whose rows without a token are zeroed in three parts: one while the tokens are sorted, one beside the windows, one beside
+    the joining. `out` holds NaN before the call; tokens lie on both sides of where the parts meet (64 MB from the front, 128 MB from the end) and at the
+    ends of their 32 and 256 rows. Every row against the fp64 sums, bounds as in test_gradient."""
+    row = K * d * (4 if odt == "f32" else 2)
+    T, first, last = 1500, (64 << 20) // row, V - (128 << 20) // row
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    tokens = torch.randint(0, V, (K, T), device="cuda", generator=gen)
+    at = [x + y for x in (0, first, first + 32, first + 256, max(first, last), V - 1) for y in (-2, -1, 0, 1)]
+    tokens[:, :len(at)] = torch.tensor(at, device="cuda")
+    tokens[:, -200:] = V // 3  # a token of more than one window
+    dY = torch.randn(K, T, d, device="cuda", generator=gen).to(DT[dt])
+    out = torch.full((K, V, d), float("nan"), device="cuda", dtype=DT[odt])
+    assert embedding.embedding_grad(dY, tokens, V, scale=0.5, out=out) is out
+    for k in range(K):
+        inside = (tokens[k] >= 0) & (tokens[k] < V)
+        ids, y = tokens[k][inside], dY[k][inside].double()
+        want = torch.zeros(V, d, device="cuda", dtype=torch.float64).index_add_(0, ids, y) * 0.5
+        size = torch.zeros(V, d, device="cuda", dtype=torch.float64).index_add_(0, ids, y.abs()) * 0.5
+        count = torch.zeros(V, 1, device="cuda", dtype=torch.float64).index_add_(0, ids, torch.ones(len(ids), 1, device="cuda", dtype=torch.float64))
+        sums = (count.clamp(min=1) + 1) * HALF["f32"] * size
+        assert ((out[k].double() - want).abs() <= sums + HALF[odt] * (want.abs() + sums)).all()
+        assert not out[k][count[:, 0] == 0].any()
