@@ -797,3 +797,69 @@ def test_parameters_as_initial_weights():
     for x in list(opt.storage.values()) + opt.W + low.W:
         assert not x.requires_grad and x.grad_fn is None
     opt.close(), low.close()
+
+
+def _bits16(key, n):
+    """ref.random16's bits on the GPU, in 64-bit integers that wrap."""
+    signed = lambda x: x - (1 << 64) if x >> 63 else x
+    shift = lambda x, s: x ^ ((x >> s) & ((1 << (64 - s)) - 1))
+    x = torch.arange(1, n // 4 + 1, device="cuda", dtype=torch.int64) * signed(0x9E3779B97F4A7C15) + signed(key)
+    x = shift(shift(x, 30) * signed(0xBF58476D1CE4E5B9), 27) * signed(0x94D049BB133111EB)
+    x = shift(x, 31)
+    return torch.stack([(x >> s) & 0xFFFF for s in (0, 16, 32, 48)], dim=1).view(-1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("w", ["f32", "bf16"])
+def test_codes_are_those_of_separately_rounded_moments(w):
+    """m's 8-bit codes, every one, are those of b1 m, a1 g and their sum each rounded to fp32 (the kernel forms pairs of them in one instruction, and a
+    compiler may fuse a product with the sum that takes it: the codes would depend on it). Codes of normal E4M3 numbers are compared: their rounding
+    is exact in fp32. 2^25 elements and three steps are enough to tell: the fused form has other codes."""
+    from oracle import lordo_oracle as lo
+    pow2 = lambda e: ((e.long() + 1023) << 52).view(torch.float64)
+    n, b1, a1 = 2 ** 25, torch.tensor(0.9, device="cuda"), torch.tensor(1.0 - 0.9, dtype=torch.float64).float().cuda()
+    opt = adamw.AdamW([torch.zeros(n, dtype=DT[w])], 1, states="8bit", seed=13)
+    coef, gen, fused_differ = torch.full((1,), 0.7, device="cuda"), torch.Generator(device="cuda").manual_seed(1), 0
+    opt.m[0].copy_(torch.randn(n, device="cuda", generator=gen).mul_(60.0).clamp_(-255.0, 255.0))
+    opt.v[0].copy_(torch.rand(n, device="cuda", generator=gen).mul_(200.0).add_(20.0))
+    opt.ms[0].view(torch.uint8).fill_(127 - 9)
+    opt.vs[0].view(torch.uint8).fill_(127 - 9)
+    for s in range(1, 4):
+        g = torch.randn(1, n, device="cuda", generator=gen).mul_(0.5).to(DT[w])
+        m0 = (opt.m[0].float().view(-1, 256) * opt.ms[0].float().view(-1, 1)).view(-1)
+        opt.step([g], 0.01, 0.9, coef=coef)
+        z = g[0].float() * coef
+        key = lo.mix64_int((lo.stream_key(13, 3, 0, s, 0) + lo._GOLDEN) & lo._MASK)
+        u = _bits16(key, n)
+        assert np.array_equal(u[:1000].cpu().numpy(), ref.random16(13, 3, s, 0, 1000))
+
+        def codes(m):
+            a = m.double().abs()
+            e = torch.frexp(a.view(-1, 256).amax(dim=1)).exponent - 8
+            t = a * pow2(-e.repeat_interleave(256))
+            step = pow2(torch.frexp(t).exponent.clamp(min=-5) - 4)
+            return torch.copysign((t / step + (u.double() + 0.5) / 65536).floor() * step, m.double()), e, t >= 2.0 ** -6
+
+        q, e, normal = codes(b1 * m0 + a1 * z)
+        assert torch.equal(opt.ms[0].view(torch.uint8).view(-1).int(), e + 127)
+        assert torch.equal(opt.m[0].view(-1).double()[normal], q[normal])
+        other = codes(((b1 * m0).double() + a1.double() * z.double()).float())[0]
+        fused_differ += int((other != q)[normal].sum())
+    assert fused_differ > 0
+    opt.close()
+
+
+@pytest.mark.gpu
+def test_moments_in_32_bits_are_rounded_operation_by_operation():
+    n = 2 ** 20 + 3
+    opt = adamw.AdamW([torch.zeros(n)], 2, beta2=0.99)
+    f32 = lambda x: torch.tensor(x, dtype=torch.float64).float().cuda()
+    b1, a1, b2, a2 = f32(0.9), f32(1.0 - 0.9), f32(0.99), f32(1.0 - 0.99)
+    coef, m, v = torch.tensor([0.7, 0.3], device="cuda"), torch.zeros(2, n, device="cuda"), torch.zeros(2, n, device="cuda")
+    for s in range(3):
+        g = gradients([(n,)], 2, s, "f32")[0]
+        opt.step([g], 0.01, 0.9, coef=coef)
+        z = g * coef.view(2, 1)
+        m, v = b1 * m + a1 * z, b2 * v + (a2 * z) * z
+        assert torch.equal(opt.m[0], m) and torch.equal(opt.v[0], v)
+    opt.close()
