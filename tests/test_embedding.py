@@ -357,3 +357,24 @@ def test_rows_without_a_token_of_a_large_table(K, V, d, dt, odt):
         sums = (count.clamp(min=1) + 1) * HALF["f32"] * size
         assert ((out[k].double() - want).abs() <= sums + HALF[odt] * (want.abs() + sums)).all()
         assert not out[k][count[:, 0] == 0].any()
+
+
+@pytest.mark.gpu
+def test_a_captured_call_on_a_forked_stream():
+    """A branch of a captured graph, its inputs recorded on the branch's stream and dropped within the capture: replayed, the eager call's bits."""
+    V, T = 300, 700
+    W = torch.randn(2, V, 24, device="cuda")
+    tok, dY = torch.randint(-1, V, (2, T), device="cuda"), torch.randn(2, T, 24, device="cuda")
+    want = embedding.embedding(W, tok, scale=2.0), embedding.embedding_grad(dY * 3.0, tok, V, K=2)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph):
+        larger = dY * 3.0
+        side.wait_stream(torch.cuda.current_stream())
+        out, grad = embedding.embedding(W, tok, scale=2.0, stream=side), embedding.embedding_grad(larger, tok, V, K=2, stream=side)
+        del larger
+        other = torch.full_like(dY, float("nan"))
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(2):
+        out.zero_(), grad.zero_()
+        graph.replay()
+        assert torch.equal(out, want[0]) and torch.equal(grad, want[1])
