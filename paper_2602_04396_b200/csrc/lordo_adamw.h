@@ -3,13 +3,14 @@
 #include <algorithm>
 
 #include "lordo_common.cuh"
+#include "lordo_plan.h"
 
 namespace lordo {
 
 constexpr int kAwBlock = 256;    // elements per scale of the 8-bit moments
-// Elements of one worker's tensor that a CTA of the step works on: 2048 (eight a thread) to 32768, about one for each of 148 * 8 CTAs where there are fewer.
+// Elements of one worker's tensor that a CTA of the step works on: 2048 (eight a thread) to 32768, about one for each of eight CTAs an SM where there are fewer.
 inline long long aw_piece(long long elements) {
-  const long long p = (elements / (148 * 8) + 2047) / 2048 * 2048;
+  const long long p = (elements / (kPlannedSms * 8) + 2047) / 2048 * 2048;
   return p < 2048 ? 2048 : p > 32768 ? 32768 : p;
 }
 constexpr int kAwOuter = 2048;   // elements of one worker's tensor that a CTA of the synchronisation works on, for all workers
