@@ -306,8 +306,8 @@ LORDO_API int64_t lordo_clip_coefficient_static_max_count(void);
  * their own, for the same K workers held as replicas, and synchronised by the same outer step (the paper's comparison systems run
  * Adam on every parameter; the low-rank path is defined for matrices only). Conventions are those at the top of this file: arrays
  * are row-major, the replica axis is outermost, device memory belongs to the caller, calls enqueue on `stream` and return.
- * Sizes need not be multiples of anything here. lordo_adamw_init and lordo_adamw_poll_status synchronise; a group's calls on different streams
- * have to be ordered by the caller.
+ * An array that a call writes overlaps no other of its arrays. Sizes need not be multiples of anything here. lordo_adamw_init and
+ * lordo_adamw_poll_status synchronise; a group's calls on different streams have to be ordered by the caller.
  * ============================================================================================= */
 
 typedef enum { LORDO_I32 = 0, LORDO_I64 = 1 } lordo_index;                     /* type of token arrays */

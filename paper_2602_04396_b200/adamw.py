@@ -207,7 +207,7 @@ class AdamW:
         self._check(self.lib.lordo_adamw_set_counters(self._ctx, (C.c_int64 * 2)(*values)), "lordo_adamw_set_counters")
 
     def clip_coefficients(self) -> torch.Tensor:
-        """[n_tensors, K] clip coefficients of the last step that formed them (copied out of the workspace)."""
+        """[n_tensors, K] clip coefficients of the last step that formed them, copied out of the workspace on the current stream."""
         ptr = C.c_void_p(None)
         self._check(self.lib.lordo_adamw_clip_coefficients(self._ctx, C.byref(ptr)), "lordo_adamw_clip_coefficients")
         off, n = ptr.value - self.workspace.data_ptr(), len(self.shapes) * self.K
